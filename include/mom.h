@@ -219,6 +219,98 @@ int mom_kv_reload(const void *pinned_host, void *k, void *v, void *stream, size_
                   void *done_event);
 
 /*
+ * Decoding in four bits: a paged KV cache, attention over it, and products with weights, all of them in elements
+ * of four bits (e2m1: sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) in blocks of 32 with
+ * a common scale 2^(b - 127) held as one byte b, 255 standing for NaN (the MXFP4 format of the Open Compute
+ * Project).  4.25 bits an element: a quarter of the bytes of the bf16 tensors, which is what a token's time goes by.
+ *
+ * What the library encodes gets the power of two that brings the largest magnitude of its block to at most 7 (between
+ * 2^-125 and 2^125), and each element the nearest code, ties to the even one: at most half a step off, nothing
+ * cut off.  A block with an infinity or a NaN becomes NaN as a whole.  Values that are read back are exact in bf16.
+ *
+ * The cache of a layer is one device buffer [pages][kv_heads] of blocks of mom_mx_block_bytes(head_dim, page_tokens)
+ * bytes, 16-byte aligned: page_tokens (16, 32, 64, 128 or 256) tokens of one key head, head_dim 64, 128 or 256.  A
+ * block of P tokens of D dimensions holds, one after the other,
+ *   key codes     [P][D / 2]              two a byte, the low nibble first
+ *   key scales    [P][D / 32]
+ *   value codes   [P / 4][16][D / 32][4]  byte (q, l, g, t): dimension 32 g + l of token 4 q + t in the low nibble,
+ *                                         32 g + 16 + l in the high one
+ *   value scales  [P / 4][D / 32][4]
+ * A page is contiguous, so mom_kv_offload and mom_kv_reload move pages as they are (two halves of a buffer as k and v).
+ * A slot is page * page_tokens + token; sequences have their pages in any order.
+ */
+size_t mom_mx_block_bytes(int64_t head_dim, int64_t page_tokens);      /* 0 for extents that are not served */
+
+/*
+ * Appends the keys and values of T tokens to the cache, keys and queries rotated by their positions on the way.
+ *   q          [T][q_heads][head_dim] bf16 in, tokens q_stride elements apart; NULL: no queries
+ *   k, v       [T][kv_heads][head_dim] bf16 in, tokens k_stride / v_stride elements apart (multiples of 8, so that the
+ *              three may be slices of one projection's output)
+ *   slots      [T] where each token goes; a token whose slot is negative or past the cache is not stored.  Two
+ *              tokens of one call must not have the same slot.
+ *   positions  [T] and inv_freq [rot_dim / 2] (fp32): pair i of the first rot_dim dimensions turns by the angle
+ *              positions[t] * inv_freq[i], (a, b) -> (a cos - b sin, b cos + a sin).  rot_dim is a multiple of 16, at most
+ *              head_dim; 0: nothing is rotated, and both may be NULL
+ *   interleaved  0: the pairs are dimensions (i, i + rot_dim / 2); else (2 i, 2 i + 1)
+ *   q_out      [T][q_heads][head_dim] bf16 out, dense; may be q itself where that is dense too
+ * The rotation runs in 64 bits: queries are rounded once, keys go from there to four bits.
+ */
+int mom_mx_kv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                     const int64_t *slots, const int32_t *positions, const float *inv_freq, int64_t rot_dim, int interleaved,
+                     int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                     void *q_out, void *cache, int64_t pages, int64_t page_tokens, void *stream);
+
+/* Tokens of the cache as the values they stand for: k, v [T][kv_heads][head_dim] bf16 out, dense; zeros for a slot
+ * that is negative or past the cache. */
+int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const int64_t *slots, int64_t T, int64_t kv_heads,
+                   int64_t head_dim, void *k, void *v, void *stream);
+
+/*
+ * Attention of T query tokens of B sequences over the cache: softmax(scale q k^T) v, q_heads / kv_heads query heads to a key head.
+ *   q            [T][q_heads][head_dim] bf16 in, tokens q_stride elements apart (a multiple of 8), rotated already
+ *   q_starts     [B + 1] device: the tokens of sequence b are q_starts[b] up to q_starts[b + 1], in order of their
+ *                positions.  NULL: T / B tokens each (T a multiple of B).  Rows of `out` that belong to no sequence are not written.
+ *   page_table   [B][table_stride] device: the pages of each sequence.  The tokens of a page that is none of the cache's
+ *                count as not seen.
+ *   kv_lens      [B] device: tokens of each sequence in the cache, the new ones among them; at most max_kv and
+ *                table_stride * page_tokens of them count
+ *   max_kv       host: no length is above it.  The work is shared out by it, so the nearer the better.
+ *   window       a token sees itself and what is before it (token i of m new ones of n stands at n - m + i), the last
+ *                `window` of those where that is not 0
+ *   out          [T][q_heads][head_dim] bf16, dense;  lse [T][q_heads] fp32 or NULL: log sum exp of the scaled scores.
+ *                A row that sees nothing is 0, its lse -infinity.
+ *   workspace    at least mom_mx_attention_workspace_bytes(T, B, q_heads, kv_heads, head_dim, max_kv) bytes, 16-byte
+ *                aligned (NULL where that is 0)
+ * Arithmetic: products of bf16 numbers with fp32 sums on the matrix cores, softmax in fp32, its weights rounded to bf16 for
+ * the second product, one rounding of the result.  What a row does not see does not reach it, NaN included.
+ */
+size_t mom_mx_attention_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_kv);
+int mom_mx_attention(const void *q, int64_t q_stride, const int32_t *q_starts, int64_t T, int64_t B,
+                     int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                     const void *cache, int64_t pages, int64_t page_tokens,
+                     const int32_t *page_table, int64_t table_stride, const int32_t *kv_lens,
+                     int64_t max_kv, float scale, int64_t window, void *out, float *lse,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* Encodes a weight w [N,K] bf16 (K a positive multiple of 32): codes [N][K / 2] (16-byte aligned), low nibble
+ * first, and scales [N][K / 32]. */
+int mom_mx_quantize(const void *w, int64_t N, int64_t K, void *codes, void *scales, void *stream);
+
+/*
+ * y = x W^T (+ residual) for one to MOM_MX_MAX_ROWS tokens and a weight in four bits, as mom_mx_quantize lays it out.
+ *   x [M,K] bf16 in;  out [M,N] fp32 (out_fp32 not 0) or bf16;  residual [M,N] bf16 or NULL, with bf16 only (may be `out` itself)
+ * fp32 sums, one rounding.  A weight in bf16 takes 3.76 times the bytes: mom_lmhead_last, mom_mlp_last.
+ */
+#define MOM_MX_MAX_ROWS 16
+int mom_mx_matvec(const void *x, int64_t M, const void *codes, const void *scales, int64_t N, int64_t K,
+                  void *out, int out_fp32, const void *residual, void *stream);
+
+/* out = silu(x W_gate^T) .* (x W_up^T), [M,N] bf16, both weights in four bits: the first half of the MLP of one to
+ * MOM_MX_MAX_ROWS tokens (mom_mx_matvec with W_down is the other).  SiLU and the product in fp32. */
+int mom_mx_gateup(const void *x, int64_t M, const void *gate_codes, const void *gate_scales,
+                  const void *up_codes, const void *up_scales, int64_t N, int64_t K, void *out, void *stream);
+
+/*
  * Testing aids (they follow no passage of the paper; process-wide, not meant for production).
  *
  * mom_debug_force_gemm_form: every later matrix-core launch uses tiles of tile_edge token rows and

@@ -6,6 +6,7 @@ built (`python -m paper_2504_12526_amd.build` or `__graft_entry__.build()`), imp
 symbols raises.
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -18,9 +19,12 @@ SYMBOLS = ("mom_status_string", "mom_mlp_workspace_bytes", "mom_mlp_prefill", "m
            "mom_lmhead_last", "mom_mlp_last", "mom_kv_offload", "mom_kv_reload",
            "mom_init", "mom_debug_force_gemm_form", "mom_debug_force_short_form", "mom_debug_force_rect_form", "mom_debug_force_block",
            "mom_mlp_prefill_static",
-           "mom_debug_mfma_probe")
+           "mom_debug_mfma_probe",
+           "mom_mx_block_bytes", "mom_mx_kv_append", "mom_mx_kv_read", "mom_mx_attention_workspace_bytes", "mom_mx_attention",
+           "mom_mx_quantize", "mom_mx_matvec", "mom_mx_gateup")
 
 MOM_STATIC_WORKSPACE_BYTES = 64 << 20
+MOM_MX_MAX_ROWS = 16
 
 (MOM_OK, MOM_ERR_NULL, MOM_ERR_SHAPE, MOM_ERR_ALIGN, MOM_ERR_ALIAS, MOM_ERR_WORKSPACE, MOM_ERR_HIP,
  MOM_ERR_HOST) = range(8)
@@ -79,6 +83,23 @@ def lib():
         L.mom_debug_force_block.argtypes = [ctypes.c_int]
         L.mom_debug_mfma_probe.restype = ctypes.c_int
         L.mom_debug_mfma_probe.argtypes = [vp, sz, vp, sz, i64, ctypes.c_int, ctypes.c_int, vp, vp]
+        L.mom_mx_block_bytes.restype = sz
+        L.mom_mx_block_bytes.argtypes = [i64, i64]
+        L.mom_mx_kv_append.restype = ctypes.c_int
+        L.mom_mx_kv_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, ctypes.c_int, i64, i64, i64, i64, vp, vp, i64, i64, vp]
+        L.mom_mx_kv_read.restype = ctypes.c_int
+        L.mom_mx_kv_read.argtypes = [vp, i64, i64, vp, i64, i64, i64, vp, vp, vp]
+        L.mom_mx_attention_workspace_bytes.restype = sz
+        L.mom_mx_attention_workspace_bytes.argtypes = [i64] * 6
+        L.mom_mx_attention.restype = ctypes.c_int
+        L.mom_mx_attention.argtypes = [vp, i64, vp, i64, i64, i64, i64, i64, vp, i64, i64, vp, i64, vp, i64, ctypes.c_float, i64,
+                                       vp, vp, vp, sz, vp]
+        L.mom_mx_quantize.restype = ctypes.c_int
+        L.mom_mx_quantize.argtypes = [vp, i64, i64, vp, vp, vp]
+        L.mom_mx_matvec.restype = ctypes.c_int
+        L.mom_mx_matvec.argtypes = [vp, i64, vp, vp, i64, i64, vp, ctypes.c_int, vp, vp]
+        L.mom_mx_gateup.restype = ctypes.c_int
+        L.mom_mx_gateup.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, vp, vp]
         _lib = L
     return _lib
 
@@ -258,4 +279,146 @@ def mom_kv_reload(pinned_host, k, v, stream, done_event=None, check=True):
                              None if done_event is None else ctypes.c_void_p(done_event.cuda_event))
     if check and rc != MOM_OK:
         raise MomError(rc, "mom_kv_reload")
+    return rc
+
+
+def _dense(name, t, dtype, shape=None):
+    if t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor" + ("" if shape is None else f" of shape {tuple(shape)}"))
+    return t
+
+
+def _tokens(name, t, width=None):
+    """[T, heads, head_dim] bf16 whose tokens may lie apart; the elements between two of them."""
+    T, heads, d = t.shape
+    if t.dtype != torch.bfloat16 or (heads > 1 and t.stride(1) != d) or t.stride(2) != 1 or (width is not None and (T, d) != width):
+        raise ValueError(f"{name} must be a bfloat16 tensor [tokens, heads, head_dim] whose heads are contiguous")
+    return t.stride(0) if T > 1 else heads * d
+
+
+def _cache(cache, page_tokens, head_dim):
+    block = mom_mx_block_bytes(head_dim, page_tokens)
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or block == 0 or cache.shape[2] != block:
+        raise ValueError("cache must be a contiguous uint8 tensor [pages, kv_heads, mom_mx_block_bytes(head_dim, page_tokens)]")
+    return cache.shape[0], cache.shape[1]
+
+
+def mom_mx_block_bytes(head_dim, page_tokens):
+    return int(lib().mom_mx_block_bytes(int(head_dim), int(page_tokens)))
+
+
+def mom_mx_kv_append(k, v, slots, cache, page_tokens, positions=None, inv_freq=None, interleaved=False, q=None, q_out=None,
+                     stream=None, check=True):
+    """k, v [T, kv_heads, head_dim] bf16 (tokens may lie apart, as slices of one projection do) into the uint8 cache
+    [pages, kv_heads, mom_mx_block_bytes] at slots [T] int64.  positions [T] int32 and inv_freq [rot_dim / 2] fp32 rotate the keys
+    and, where given, the queries q [T, q_heads, head_dim] into q_out."""
+    T, kv_heads, d = k.shape
+    pages, heads = _cache(cache, page_tokens, d)
+    if tuple(v.shape) != tuple(k.shape) or heads != kv_heads:
+        raise ValueError("k and v must have the same shape and the cache their heads")
+    if (positions is None) != (inv_freq is None) or (q is None) != (q_out is None):
+        raise ValueError("positions and inv_freq, q and q_out come together")
+    strides = _tokens("k", k), _tokens("v", v)
+    _dense("slots", slots, torch.int64, (T,))
+    rot = 0
+    if inv_freq is not None:
+        _dense("positions", positions, torch.int32, (T,))
+        rot = 2 * _dense("inv_freq", inv_freq, torch.float32).numel()
+    q_stride = q_heads = 0
+    if q is not None:
+        q_stride, q_heads = _tokens("q", q, (T, d)), q.shape[1]
+        _dense("q_out", q_out, torch.bfloat16, q.shape)
+    rc = lib().mom_mx_kv_append(_ptr(q), q_stride, _ptr(k), strides[0], _ptr(v), strides[1], _ptr(slots), _ptr(positions if rot else None),
+                                _ptr(inv_freq if rot else None), rot, int(bool(interleaved)), T, q_heads, kv_heads, d, _ptr(q_out), _ptr(cache), pages,
+                                int(page_tokens), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_kv_append")
+    return rc
+
+
+def mom_mx_kv_read(cache, page_tokens, slots, k, v, stream=None, check=True):
+    """The tokens at slots [T] int64 as k, v [T, kv_heads, head_dim] bf16."""
+    T, kv_heads, d = k.shape
+    pages, heads = _cache(cache, page_tokens, d)
+    _dense("slots", slots, torch.int64, (T,))
+    _dense("k", k, torch.bfloat16, (T, heads, d))
+    _dense("v", v, torch.bfloat16, (T, heads, d))
+    rc = lib().mom_mx_kv_read(_ptr(cache), pages, int(page_tokens), _ptr(slots), T, kv_heads, d, _ptr(k), _ptr(v), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_kv_read")
+    return rc
+
+
+def mom_mx_attention_workspace_bytes(T, B, q_heads, kv_heads, head_dim, max_kv):
+    return int(lib().mom_mx_attention_workspace_bytes(int(T), int(B), int(q_heads), int(kv_heads), int(head_dim), int(max_kv)))
+
+
+def mom_mx_attention(q, cache, page_tokens, page_table, kv_lens, max_kv, out, workspace, q_starts=None, scale=None, window=0, lse=None,
+                     stream=None, check=True):
+    """q [T, q_heads, head_dim] bf16 (tokens may lie apart) of B sequences over the cache: page_table [B, n] int32 (rows may lie
+    apart), kv_lens [B] int32, q_starts [B + 1] int32 or None (T / B tokens each), scale None: 1 / sqrt(head_dim).  out like q, dense;
+    lse [T, q_heads] fp32 or None; workspace any device tensor of at least mom_mx_attention_workspace_bytes bytes, or None where that is 0."""
+    T, q_heads, d = q.shape
+    pages, kv_heads = _cache(cache, page_tokens, d)
+    B, each = page_table.shape
+    if page_table.dtype != torch.int32 or (each > 1 and page_table.stride(1) != 1) or (B > 1 and page_table.stride(0) < each):
+        raise ValueError("page_table must be an int32 tensor [B, n] with contiguous rows")
+    # rows that lie apart are passed as one that is as long as their distance, and what lies between them stays out of reach through max_kv
+    table_stride = page_table.stride(0) if B > 1 else each
+    _dense("kv_lens", kv_lens, torch.int32, (B,))
+    if q_starts is not None:
+        _dense("q_starts", q_starts, torch.int32, (B + 1,))
+    _dense("out", out, torch.bfloat16, q.shape)
+    if lse is not None:
+        _dense("lse", lse, torch.float32, (T, q_heads))
+    rc = lib().mom_mx_attention(_ptr(q), _tokens("q", q), _ptr(q_starts), T, B, q_heads, kv_heads, d, _ptr(cache), pages, int(page_tokens),
+                                _ptr(page_table), table_stride, _ptr(kv_lens), min(int(max_kv), each * int(page_tokens)),
+                                1.0 / math.sqrt(d) if scale is None else float(scale), int(window), _ptr(out), _ptr(lse),
+                                _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_attention")
+    return rc
+
+
+def mom_mx_quantize(w, codes, scales, stream=None, check=True):
+    """w [N, K] bf16 into codes [N, K / 2] and scales [N, K / 32] (uint8)."""
+    N, K = w.shape
+    _dense("w", w, torch.bfloat16)
+    _dense("codes", codes, torch.uint8, (N, K // 2))
+    _dense("scales", scales, torch.uint8, (N, K // 32))
+    rc = lib().mom_mx_quantize(_ptr(w), N, K, _ptr(codes), _ptr(scales), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_quantize")
+    return rc
+
+
+def mom_mx_matvec(x, codes, scales, out, residual=None, stream=None, check=True):
+    """x [M, K] bf16 times the weight in four bits, codes [N, K / 2] and scales [N, K / 32]: out [M, N] fp32, or bf16 with
+    residual [M, N] bf16 added where given."""
+    M, K = x.shape
+    N = codes.shape[0]
+    _dense("x", x, torch.bfloat16)
+    _dense("codes", codes, torch.uint8, (N, K // 2))
+    _dense("scales", scales, torch.uint8, (N, K // 32))
+    _dense("out", out, torch.float32 if out.dtype == torch.float32 else torch.bfloat16, (M, N))
+    if residual is not None:
+        _dense("residual", residual, torch.bfloat16, (M, N))
+    rc = lib().mom_mx_matvec(_ptr(x), M, _ptr(codes), _ptr(scales), N, K, _ptr(out), int(out.dtype == torch.float32), _ptr(residual), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_matvec")
+    return rc
+
+
+def mom_mx_gateup(x, gate_codes, gate_scales, up_codes, up_scales, out, stream=None, check=True):
+    """silu(x W_gate^T) * (x W_up^T) for x [M, K] bf16 and two weights [N, K] in four bits: out [M, N] bf16."""
+    M, K = x.shape
+    N = gate_codes.shape[0]
+    _dense("x", x, torch.bfloat16)
+    for name, c, s in (("gate", gate_codes, gate_scales), ("up", up_codes, up_scales)):
+        _dense(name + "_codes", c, torch.uint8, (N, K // 2))
+        _dense(name + "_scales", s, torch.uint8, (N, K // 32))
+    _dense("out", out, torch.bfloat16, (M, N))
+    rc = lib().mom_mx_gateup(_ptr(x), M, _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes), _ptr(up_scales), N, K, _ptr(out), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_gateup")
     return rc

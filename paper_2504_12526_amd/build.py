@@ -12,6 +12,8 @@ DEPS = SOURCES + [os.path.join(CSRC, "mom_gemm.hip.inc"), os.path.join(CSRC, "mo
                   os.path.join(CSRC, "mom_block.hip.inc"), os.path.join(CSRC, "mom_kv.hip.inc"),
                   os.path.join(CSRC, "mom_gemm_forms.h"), os.path.join(CSRC, "mom_gemm_schedule.h"),
                   os.path.join(CSRC, "mom_gemv.hip.inc"), os.path.join(CSRC, "mom_probe.hip.inc"),
+                  os.path.join(CSRC, "mom_mx.h"), os.path.join(CSRC, "mom_mx_kv.hip.inc"), os.path.join(CSRC, "mom_mx_attention.hip.inc"),
+                  os.path.join(CSRC, "mom_mx_matvec.hip.inc"), os.path.join(CSRC, "mom_mx_calls.hip.inc"),
                   os.path.join(ROOT, "include", "mom.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <initializer_list>
 #include <tuple>
 #include <type_traits>
 
@@ -22,6 +23,10 @@
 #include "mom_gemv.hip.inc"
 #include "mom_kv.hip.inc"
 #include "mom_probe.hip.inc"
+#include "mom_mx.h"
+#include "mom_mx_kv.hip.inc"
+#include "mom_mx_attention.hip.inc"
+#include "mom_mx_matvec.hip.inc"
 
 // Workspace of mom_mlp_prefill_static: one copy per device, held from the moment the library is
 // loaded on a device until the process ends.  In host code this name is only a handle for
@@ -676,3 +681,5 @@ int mom_kv_reload(const void* pinned_host, void* k, void* v, void* stream, size_
 }
 
 }  // extern "C"
+
+#include "mom_mx_calls.hip.inc"

@@ -1,0 +1,189 @@
+// Four-bit elements in blocks of 32 with a common power of two (OCP Microscaling: e2m1 elements, one e8m0 scale): their encoding, the layout
+// of a block of the paged cache, and how attention over it is cut into tiles and shares, as kernels (mom_mx_*.hip.inc), entry points and a
+// host program (tests/mx_check.cpp) ask.  Plain C++17, no HIP types.
+//
+// A code is sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; a scale byte b stands for 2^(b - 127),
+// 255 for NaN.  gfx950 turns two codes and a scale into two bf16 numbers in one instruction, exactly (8 significant bits hold every product), so
+// nothing is rounded between the cache and the matrix cores.
+#ifndef MOM_MX_H
+#define MOM_MX_H
+
+#include <stddef.h>
+#include <stdint.h>
+#include <string.h>
+
+#if defined(__HIPCC__)
+#define MOM_MX_FN __host__ __device__ inline
+#else
+#define MOM_MX_FN inline
+#endif
+
+namespace momk {
+namespace mx {
+
+constexpr int kBlock = 32;                              // elements of a block
+constexpr int kScaleNaN = 255;
+constexpr int kMinExponent = -125, kMaxExponent = 125;  // of a scale that the library writes: every nonzero value is a normal bf16 number then
+
+// ---- encoding -------------------------------------------------------------------------------------------------------------
+
+// What encodes a number: its magnitude as bits (which order like the magnitudes, infinities and NaN last) and the parts of them.
+struct F32 {
+    typedef float value;
+    typedef uint32_t bits;
+    static constexpr int kMantissa = 23, kBias = 127;
+};
+struct F64 {
+    typedef double value;
+    typedef uint64_t bits;
+    static constexpr int kMantissa = 52, kBias = 1023;
+};
+
+template <class F>
+MOM_MX_FN typename F::bits magnitude_bits(typename F::value x) {
+    typename F::bits b;
+    memcpy(&b, &x, sizeof b);
+    return b << 1 >> 1;
+}
+template <class F>
+MOM_MX_FN bool finite(typename F::bits magnitude) {
+    return (magnitude >> F::kMantissa) < (typename F::bits)(2 * F::kBias + 1);
+}
+
+// Exponent of the scale of a block whose largest magnitude is `top` (finite): the power of two that brings it to at most 7, which is half a step
+// away from the largest element 6, so that no element is further than half a step from its code (the rounding down to [4, 8) that is
+// also in use cuts off up to a quarter of the largest element).
+template <class F>
+MOM_MX_FN int scale_exponent(typename F::bits top) {
+    const typename F::bits fraction = top & (((typename F::bits)1 << F::kMantissa) - 1);
+    const int e = (int)(top >> F::kMantissa) - F::kBias - 2 + (fraction > ((typename F::bits)3 << (F::kMantissa - 2)) ? 1 : 0);
+    return e < kMinExponent ? kMinExponent : e > kMaxExponent ? kMaxExponent : e;
+}
+
+// 2^-e for the exponent of a scale.
+template <class F>
+MOM_MX_FN typename F::value inverse_scale(int e) {
+    const typename F::bits b = (typename F::bits)(F::kBias - e) << F::kMantissa;
+    typename F::value v;
+    memcpy(&v, &b, sizeof v);
+    return v;
+}
+
+// The code of x, `inverse` from inverse_scale: the nearest element, ties to the even code, above 6 the largest.
+template <class F>
+MOM_MX_FN uint32_t encode(typename F::value x, typename F::value inverse) {
+    typedef typename F::value V;
+    const V a = (x < 0 ? -x : x) * inverse;             // exact: a power of two
+    return (uint32_t)(a > (V)0.25) + (uint32_t)(a >= (V)0.75) + (uint32_t)(a > (V)1.25) + (uint32_t)(a >= (V)1.75) + (uint32_t)(a > (V)2.5) +
+           (uint32_t)(a >= (V)3.5) + (uint32_t)(a > (V)5.0) + (x < 0 ? 8u : 0u);
+}
+
+// ---- layout of the paged cache --------------------------------------------------------------------------------------------
+
+// A page holds P tokens for every key head, a block of block_bytes each:
+//     key codes     [P][D / 2]            low nibble first
+//     key scales    [P][D / 32]
+//     value codes   [P / 4][16][D / 32][4]   byte (q, l, g, t): dimension 32 g + l of token 4 q + t, and 32 g + 16 + l in the high nibble
+//     value scales  [P / 4][D / 32][4]
+// Keys are contracted over the dimensions and values over the tokens, and a lane of the matrix cores takes neighbours along the contracted
+// axis: so a lane's operand of either is one run of bytes, and a wavefront's loads of 16 tokens are contiguous.
+MOM_MX_FN size_t block_bytes(int P, int D) { return (size_t)P * (size_t)(D + D / 16); }
+MOM_MX_FN int key_codes(int D, int at) { return at * (D / 2); }
+MOM_MX_FN int key_scales(int P, int D, int at) { return P * (D / 2) + at * (D / 32); }
+MOM_MX_FN int value_codes(int P, int D, int quad) { return P * (D / 2 + D / 32) + quad * 2 * D; }
+MOM_MX_FN int value_scales(int P, int D, int quad) { return P * (D + D / 32) + quad * (D / 8); }
+
+MOM_MX_FN bool head_dim_served(int64_t D) { return D == 64 || D == 128 || D == 256; }
+MOM_MX_FN bool page_served(int64_t P) { return P >= 16 && P <= 256 && (P & (P - 1)) == 0; }
+
+// ---- tiles of attention ---------------------------------------------------------------------------------------------------
+
+// The query rows of a sequence at one key head, `group` query heads for each of its tokens, are cut into tiles of `rows`.  Where the tokens of a
+// sequence start is known on the device only, so tiles are numbered such that the number of sequence b's first one needs nothing but
+// its start: floor(start * group / rows) + b leaves each at least as many numbers as it has tiles.
+MOM_MX_FN int64_t first_tile(int64_t start, int64_t b, int group, int rows) { return start * group / rows + b; }
+MOM_MX_FN int64_t tile_numbers(int64_t T, int64_t B, int group, int rows) { return T * group / rows + B; }
+
+// The sequence of tile `number`, and which of its tiles it is; b = -1 where the number is no tile's.  Where every sequence has m tokens, and
+// where b is the last whose first number is not behind `number` (0 if there is none).
+struct Tile { int b, tile; };
+MOM_MX_FN Tile checked_tile(int64_t b, int64_t tile, int64_t B, int64_t m, int group, int rows) {
+    if (b >= B || tile < 0 || tile * rows >= m * group) return {-1, 0};
+    return {(int)b, (int)tile};
+}
+MOM_MX_FN Tile even_tile(int64_t number, int64_t B, int64_t m, int group, int rows) {
+    const int64_t tiles = (m * group + rows - 1) / rows, b = number / tiles;
+    return checked_tile(b, number - b * tiles, B, m, group, rows);
+}
+MOM_MX_FN Tile listed_tile(int64_t number, int64_t b, int64_t start, int64_t B, int64_t m, int group, int rows) {
+    return checked_tile(b, number - first_tile(start, b, group, rows), B, m, group, rows);
+}
+
+// The tokens of the cache that the rows of a tile see: tokens [first, last] of the sequence's m new ones, n in the cache.  Token i stands at
+// n - m + i, sees itself and what is before it, and not what is `window` or more before it (0: no window).
+struct Span { int lo, hi; };                            // tokens [lo, hi)
+MOM_MX_FN Span tile_span(int n, int m, int first, int last, int window) {
+    const int64_t p0 = (int64_t)n - m + first, p1 = (int64_t)n - m + last;         // p1 < n
+    int64_t lo = window > 0 ? p0 - window + 1 : 0, hi = p1 + 1;
+    if (lo < 0) lo = 0;
+    if (hi <= lo) return {0, 0};
+    return {(int)lo, (int)hi};
+}
+
+// A step of a wavefront is kStep tokens at a multiple of it, and a share (one workgroup's part of a tile's tokens) `share` of them from the
+// step that has the first visible token.
+constexpr int kStep = 32;
+MOM_MX_FN Span share_span(Span s, int64_t z, int64_t share) {
+    const int64_t base = s.lo / kStep * kStep, lo = base + z * share, hi = lo + share;
+    const int64_t a = lo > s.lo ? lo : s.lo, b = hi < s.hi ? hi : s.hi;
+    if (b <= a) return {0, 0};
+    return {(int)a, (int)b};
+}
+
+// Tokens that a tile can reach: the rows of `rows / group` tokens (and the two that a tile may cut), their window, and what lies in front of
+// the first in its step.
+MOM_MX_FN int64_t tile_reach(int64_t max_kv, int64_t window, int group, int rows) {
+    if (window <= 0) return max_kv;
+    const int64_t r = window + rows / group + 2 + kStep;
+    return r < max_kv ? r : max_kv;
+}
+
+// How a call is launched: tiles of `rows` query rows (16 qb for each of the workgroup's four wavefronts, or for all four, who share the tokens then:
+// `split`), and the tokens of a tile in `shares` of `share`.
+struct AttentionPlan {
+    int qb, split, rows, shares;
+    int64_t share, numbers;
+};
+constexpr int kWorkgroups = 1024;       // that the tokens are shared out for: four for each of 256 compute units
+constexpr int kLeastShare = 256;        // tokens
+
+MOM_MX_FN int64_t most_shares(int64_t reach, int64_t workgroups) {
+    const int64_t want = (kWorkgroups + workgroups - 1) / workgroups, least = (reach + kLeastShare - 1) / kLeastShare;
+    const int64_t s = want < least ? want : least;
+    return s < 1 ? 1 : s;
+}
+MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, int64_t max_kv, int64_t window) {
+    const int group = Hq / Hkv;
+    const int64_t average = T * group / B;
+    AttentionPlan p;
+    p.qb = average <= 16 ? 1 : 2;
+    p.split = average <= 64;
+    p.rows = 16 * p.qb * (p.split ? 1 : 4);
+    p.numbers = tile_numbers(T, B, group, p.rows);
+    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, p.numbers * Hkv);
+    p.share = ((reach + s - 1) / s + kStep - 1) / kStep * kStep;
+    if (p.share < kStep) p.share = kStep;
+    p.shares = reach > 0 ? (int)((reach + p.share - 1) / p.share) : 1;
+    return p;
+}
+// Bytes of workspace: for every share of every row its sums, maximum and sum of weights.  A window leaves fewer shares, never more.
+MOM_MX_FN size_t attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
+    const AttentionPlan p = attention_plan(T, B, Hq, Hkv, max_kv, 0);
+    const int64_t s = most_shares(max_kv, p.numbers * Hkv);
+    return s <= 1 ? 0 : (size_t)s * (size_t)T * (size_t)Hq * (size_t)(D + 2) * 4;
+}
+
+}  // namespace mx
+}  // namespace momk
+
+#endif
