@@ -292,7 +292,7 @@ int mom_mx_attention(const void *q, int64_t q_stride, const int32_t *q_starts, i
                      int64_t max_kv, float scale, int64_t window, void *out, float *lse,
                      void *workspace, size_t workspace_bytes, void *stream);
 
-/* Encodes a weight w [N,K] bf16 (K a positive multiple of 32): codes [N][K / 2] (16-byte aligned), low nibble
+/* Encodes a weight w [N,K] bf16 (K a positive multiple of 32, at most 32768): codes [N][K / 2] (16-byte aligned), low nibble
  * first, and scales [N][K / 32]. */
 int mom_mx_quantize(const void *w, int64_t N, int64_t K, void *codes, void *scales, void *stream);
 

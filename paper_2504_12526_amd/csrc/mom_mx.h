@@ -101,43 +101,48 @@ MOM_MX_FN bool page_served(int64_t P) { return P >= 16 && P <= 256 && (P & (P - 
 // The query rows of a sequence at one key head, `group` query heads for each of its tokens, are cut into tiles of `rows`.  Where the tokens of a
 // sequence start is known on the device only, so tiles are numbered such that the number of sequence b's first one needs nothing but
 // its start: floor(start * group / rows) + b leaves each at least as many numbers as it has tiles.
-MOM_MX_FN int64_t first_tile(int64_t start, int64_t b, int group, int rows) { return start * group / rows + b; }
+// (32 bits hold all of it: up to 2^29 tokens and 2^31 rows of queries.)
+MOM_MX_FN uint32_t first_tile(uint32_t start, uint32_t b, uint32_t group, uint32_t rows) { return start * group / rows + b; }
 MOM_MX_FN int64_t tile_numbers(int64_t T, int64_t B, int group, int rows) { return T * group / rows + B; }
 
 // The sequence of tile `number`, and which of its tiles it is; b = -1 where the number is no tile's.  Where every sequence has m tokens, and
 // where b is the last whose first number is not behind `number` (0 if there is none).
 struct Tile { int b, tile; };
-MOM_MX_FN Tile checked_tile(int64_t b, int64_t tile, int64_t B, int64_t m, int group, int rows) {
-    if (b >= B || tile < 0 || tile * rows >= m * group) return {-1, 0};
-    return {(int)b, (int)tile};
+MOM_MX_FN Tile checked_tile(uint32_t b, int tile, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
+    if (b >= B || tile < 0 || (uint32_t)tile >= (m * group + rows - 1) / rows) return {-1, 0};
+    return {(int)b, tile};
 }
-MOM_MX_FN Tile even_tile(int64_t number, int64_t B, int64_t m, int group, int rows) {
-    const int64_t tiles = (m * group + rows - 1) / rows, b = number / tiles;
-    return checked_tile(b, number - b * tiles, B, m, group, rows);
+MOM_MX_FN Tile even_tile(uint32_t number, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
+    const uint32_t tiles = (m * group + rows - 1) / rows, b = tiles == 1 ? number : number / tiles;
+    return checked_tile(b, (int)(number - b * tiles), B, m, group, rows);
 }
-MOM_MX_FN Tile listed_tile(int64_t number, int64_t b, int64_t start, int64_t B, int64_t m, int group, int rows) {
-    return checked_tile(b, number - first_tile(start, b, group, rows), B, m, group, rows);
+MOM_MX_FN Tile listed_tile(uint32_t number, uint32_t b, uint32_t start, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
+    return checked_tile(b, (int)(number - first_tile(start, b, group, rows)), B, m, group, rows);
 }
+
+// r / group for r < 2^16 + 2^15 and group < 2^15, by a multiplication: inverse = floor(2^32 / group) + 1 is off by less than 1 in 2^32 / group of it.
+MOM_MX_FN uint32_t inverse_of(uint32_t group) { return group == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / group) + 1; }
+MOM_MX_FN uint32_t divided(uint32_t r, uint32_t inverse) { return inverse ? (uint32_t)(((uint64_t)r * inverse) >> 32) : r; }
 
 // The tokens of the cache that the rows of a tile see: tokens [first, last] of the sequence's m new ones, n in the cache.  Token i stands at
 // n - m + i, sees itself and what is before it, and not what is `window` or more before it (0: no window).
 struct Span { int lo, hi; };                            // tokens [lo, hi)
 MOM_MX_FN Span tile_span(int n, int m, int first, int last, int window) {
-    const int64_t p0 = (int64_t)n - m + first, p1 = (int64_t)n - m + last;         // p1 < n
-    int64_t lo = window > 0 ? p0 - window + 1 : 0, hi = p1 + 1;
+    const int p0 = n - m + first, p1 = n - m + last;                                 // p1 < n
+    int lo = window > 0 ? p0 - window + 1 : 0, hi = p1 + 1;
     if (lo < 0) lo = 0;
     if (hi <= lo) return {0, 0};
-    return {(int)lo, (int)hi};
+    return {lo, hi};
 }
 
 // A step of a wavefront is kStep tokens at a multiple of it, and a share (one workgroup's part of a tile's tokens) `share` of them from the
 // step that has the first visible token.
 constexpr int kStep = 32;
-MOM_MX_FN Span share_span(Span s, int64_t z, int64_t share) {
-    const int64_t base = s.lo / kStep * kStep, lo = base + z * share, hi = lo + share;
-    const int64_t a = lo > s.lo ? lo : s.lo, b = hi < s.hi ? hi : s.hi;
+MOM_MX_FN Span share_span(Span s, int z, int share) {
+    const int base = s.lo / kStep * kStep, lo = base + z * share, hi = lo + share;
+    const int a = lo > s.lo ? lo : s.lo, b = hi < s.hi ? hi : s.hi;
     if (b <= a) return {0, 0};
-    return {(int)a, (int)b};
+    return {a, b};
 }
 
 // Tokens that a tile can reach: the rows of `rows / group` tokens (and the two that a tile may cut), their window, and what lies in front of
@@ -148,29 +153,47 @@ MOM_MX_FN int64_t tile_reach(int64_t max_kv, int64_t window, int group, int rows
     return r < max_kv ? r : max_kv;
 }
 
-// How a call is launched: tiles of `rows` query rows (16 qb for each of the workgroup's four wavefronts, or for all four, who share the tokens then:
-// `split`), and the tokens of a tile in `shares` of `share`.
+// How a call is launched: tiles of `rows` query rows, 16 qb for each wavefront; `wk` wavefronts have the same rows and share their tokens (1: each of
+// four has its own); the tokens of a tile in `shares` of `share`, which mx_join_kernel joins.
 struct AttentionPlan {
-    int qb, split, rows, shares;
+    int qb, wk, rows, shares;
     int64_t share, numbers;
 };
-constexpr int kWorkgroups = 1024;       // that the tokens are shared out for: four for each of 256 compute units
-constexpr int kLeastShare = 256;        // tokens
+MOM_MX_FN constexpr int tile_rows(int qb, int wk) { return 16 * qb * (wk > 1 ? 1 : 4); }
 
-MOM_MX_FN int64_t most_shares(int64_t reach, int64_t workgroups) {
-    const int64_t want = (kWorkgroups + workgroups - 1) / workgroups, least = (reach + kLeastShare - 1) / kLeastShare;
+// Wavefronts that share a tile's tokens where workgroups are few: what the registers of a compute unit hold of them (qb = 1 takes up to 128 registers
+// a lane with 64 and 128 dimensions and up to 256 with 256, qb = 2 twice that).
+MOM_MX_FN constexpr int wide(int qb, int D) { return qb == 1 ? (D == 256 ? 8 : 16) : (D == 256 ? 4 : 8); }
+#ifndef WGN
+#define WGN 1024
+#endif
+#ifndef WGW
+#define WGW 256
+#endif
+#ifndef LSH
+#define LSH 2
+#endif
+constexpr int kManyWorkgroups = WGN;    // so many, of four wavefronts, fill the device and need not be wide
+constexpr int kWorkgroups = WGW;        // that the tokens are shared out for: the compute units
+constexpr int kLeastSteps = LSH;          // of a wavefront that a share is worth its joining for
+
+// Shares of a tile of `reach` tokens with `workgroups` tiles; more for longer reaches, never fewer.
+MOM_MX_FN int64_t most_shares(int64_t reach, int64_t workgroups, int wk) {
+    const int64_t want = kWorkgroups / workgroups, least = (reach + kLeastSteps * wk * kStep - 1) / (kLeastSteps * wk * kStep);
     const int64_t s = want < least ? want : least;
     return s < 1 ? 1 : s;
 }
-MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, int64_t max_kv, int64_t window) {
+MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window) {
     const int group = Hq / Hkv;
-    const int64_t average = T * group / B;
+    const int64_t average = (T * group + B - 1) / B;
     AttentionPlan p;
     p.qb = average <= 16 ? 1 : 2;
-    p.split = average <= 64;
-    p.rows = 16 * p.qb * (p.split ? 1 : 4);
+    p.wk = average > 64 ? 1 : wide(p.qb, D);
+    const int64_t workgroups = B * ((average + tile_rows(p.qb, p.wk) - 1) / tile_rows(p.qb, p.wk)) * Hkv;
+    if (p.qb == 1 && workgroups >= kManyWorkgroups) p.wk = 4;
+    p.rows = tile_rows(p.qb, p.wk);
     p.numbers = tile_numbers(T, B, group, p.rows);
-    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, p.numbers * Hkv);
+    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, workgroups, p.wk);
     p.share = ((reach + s - 1) / s + kStep - 1) / kStep * kStep;
     if (p.share < kStep) p.share = kStep;
     p.shares = reach > 0 ? (int)((reach + p.share - 1) / p.share) : 1;
@@ -178,8 +201,8 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
 }
 // Bytes of workspace: for every share of every row its sums, maximum and sum of weights.  A window leaves fewer shares, never more.
 MOM_MX_FN size_t attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
-    const AttentionPlan p = attention_plan(T, B, Hq, Hkv, max_kv, 0);
-    const int64_t s = most_shares(max_kv, p.numbers * Hkv);
+    const AttentionPlan p = attention_plan(T, B, Hq, Hkv, D, max_kv, 0);
+    const int64_t average = (T * (Hq / Hkv) + B - 1) / B, s = most_shares(max_kv, B * ((average + p.rows - 1) / p.rows) * Hkv, p.wk);
     return s <= 1 ? 0 : (size_t)s * (size_t)T * (size_t)Hq * (size_t)(D + 2) * 4;
 }
 

@@ -152,31 +152,31 @@ static void numbers(std::mt19937& rng) {
 }
 
 static void tokens(std::mt19937& rng) {
-    const int Hkv = 1 << (rng() % 4), group = 1 + rng() % 8, page = 16 << (rng() % 5);
+    const int D = 64 << (rng() % 3), Hkv = 1 << (rng() % 4), group = 1 + rng() % 8, page = 16 << (rng() % 5);
     const int B = 1 + rng() % 8, m = 1 + rng() % (rng() % 2 ? 4 : 400);
     const int max_kv = rng() % (rng() % 2 ? 300 : 40000), window = rng() % 2 ? 0 : 1 + rng() % 3000;
     const int n = max_kv ? rng() % (max_kv + 1) : 0;
-    const mx::AttentionPlan p = mx::attention_plan((int64_t)B * m, B, Hkv * group, Hkv, max_kv, window);
+    const mx::AttentionPlan p = mx::attention_plan((int64_t)B * m, B, Hkv * group, Hkv, D, max_kv, window);
     CHECK(p.share % mx::kStep == 0 && p.share > 0 && p.shares >= 1, "share %lld", (long long)p.share);
     if (p.shares > 1) {
-        const size_t need = (size_t)p.shares * B * m * Hkv * group * (128 + 2) * 4, have = mx::attention_workspace((int64_t)B * m, B, Hkv * group, Hkv, 128, max_kv);
+        const size_t need = (size_t)p.shares * B * m * Hkv * group * (D + 2) * 4, have = mx::attention_workspace((int64_t)B * m, B, Hkv * group, Hkv, D, max_kv);
         CHECK(need <= have, "workspace %zu of %zu", need, have);
     }
     const int all = m * group, table = (max_kv + page - 1) / page;
     const int tile = rng() % ((all + p.rows - 1) / p.rows);
     const int last_row = std::min((tile + 1) * p.rows, all) - 1;
     const mx::Span whole = mx::tile_span(n, m, tile * p.rows / group, last_row / group, window);
-    for (int wave = 0; wave < 4; ++wave) {
-        const int row0 = tile * p.rows + (p.split ? 0 : wave * 16 * p.qb);
+    for (int wave = 0; wave < (p.wk > 1 ? 1 : 4); ++wave) {
+        const int row0 = tile * p.rows + wave * 16 * p.qb;
         if (row0 >= all) continue;
         const int last = std::min(row0 + 16 * p.qb, all) - 1;
         const mx::Span seen = mx::tile_span(n, m, row0 / group, last / group, window);
         std::vector<int> taken(n + 1, 0);
         for (int z = 0; z < p.shares; ++z) {
             const mx::Span part = mx::share_span(whole, z, p.share);
-            const int lo = std::max(part.lo, seen.lo), hi = std::min(part.hi, seen.hi), WK = p.split ? 4 : 1;
+            const int lo = std::max(part.lo, seen.lo), hi = std::min(part.hi, seen.hi), WK = p.wk;
             for (int w = 0; w < WK; ++w) {
-                const int token0 = lo / mx::kStep * mx::kStep + (WK == 4 ? w * mx::kStep : 0);
+                const int token0 = lo / mx::kStep * mx::kStep + (WK > 1 ? w * mx::kStep : 0);
                 const int steps = hi > token0 ? (hi - token0 + WK * mx::kStep - 1) / (WK * mx::kStep) : 0;
                 for (int step = 0; step < steps; ++step)
                     for (int i = 0; i < mx::kStep; ++i) {
@@ -211,6 +211,9 @@ int main() {
     std::mt19937 rng(7);
     encoding<mx::F32>(rng);
     encoding<mx::F64>(rng);
+    for (uint32_t group = 1; group < (1 << 15); group += group < 300 ? 1 : 977)
+        for (uint32_t r = 0; r < (1 << 16) + (1 << 15); r += r < 2000 ? 1 : 313)
+            CHECK(mx::divided(r, mx::inverse_of(group)) == r / group, "divided: %u / %u", r, group);
     for (int i = 0; i < 3000; ++i) numbers(rng);
     for (int i = 0; i < 3000; ++i) tokens(rng);
     if (!bad) std::printf("four-bit layout, encoding, tiles and shares: ok\n");

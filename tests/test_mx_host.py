@@ -35,11 +35,12 @@ def test_layout_encoding_tiles_and_shares(tmp_path):
     ("(a >= (V)1.75)", "(a > (V)1.75)", "nearer"),
     ("(uint32_t)(a > (V)2.5)", "(uint32_t)(a >= (V)2.5)", "nearer"),
     ("kBias - 2 + (fraction", "kBias - 3 + (fraction", "scale"),
-    ("return start * group / rows + b;", "return start * group / rows;", "number"),
+    ("{ return start * group / rows + b; }", "{ return start * group / rows; }", "number"),
     ("if (b >= B || tile < 0", "if (tile < 0", "sequence"),
-    ("tile * rows >= m * group", "tile * rows >= m * group + rows", "number"),
+    ("(uint32_t)tile >= (m * group + rows - 1) / rows)", "(uint32_t)tile > (m * group + rows - 1) / rows)", "number"),
+    ("/ group) + 1;", "/ group);", "divided"),
     ("hi = p1 + 1;", "hi = p1;", "taken"),
-    ("const int64_t base = s.lo / kStep * kStep,", "const int64_t base = s.lo / kStep * kStep + kStep,", "taken"),
+    ("const int base = s.lo / kStep * kStep,", "const int base = s.lo / kStep * kStep + kStep,", "taken"),
     ("const int64_t r = window + rows / group + 2 + kStep;", "const int64_t r = window;", "taken"),
 ])
 def test_a_planted_mistake_is_caught(tmp_path, old, new, says):
@@ -160,7 +161,7 @@ def test_products_refuse_before_any_launch():
         return L.mom_mx_quantize(vp(w), N, K, vp(c), vp(s), None)
 
     for call in (mv, gu):
-        for bad in (dict(M=-1), dict(M=binding.MOM_MX_MAX_ROWS + 1), dict(N=-1), dict(K=0), dict(K=48), dict(K=1 << 21)):
+        for bad in (dict(M=-1), dict(M=binding.MOM_MX_MAX_ROWS + 1), dict(N=-1), dict(K=0), dict(K=48), dict(K=32768 + 32)):
             assert call(**bad) == SHAPE, bad
         assert call(M=0) == OK and call(N=0) == OK
         for bad in (dict(x=0), dict(out=0)):
@@ -171,7 +172,7 @@ def test_products_refuse_before_any_launch():
             assert call(**bad) == ALIAS, bad
     assert mv(fp32=1) == SHAPE and mv(c=0) == NULL and mv(s=0) == NULL and mv(c=A[1] + 8) == ALIGN and mv(res=A[4] + 8) == ALIGN and mv(res=A[3] + 16) == ALIAS
     assert gu(gc=0) == NULL and gu(us=0) == NULL and gu(uc=A[3] + 4) == ALIGN and gu(out=A[3] + 16) == ALIAS and gu(out=A[4] + 16) == ALIAS
-    assert qu(N=-1) == SHAPE and qu(K=33) == SHAPE and qu(N=0) == OK
+    assert qu(N=-1) == SHAPE and qu(K=33) == SHAPE and qu(K=32800) == SHAPE and qu(N=0) == OK
     assert qu(w=0) == NULL and qu(c=0) == NULL and qu(s=0) == NULL and qu(w=A[0] + 2) == ALIGN and qu(c=A[1] + 4) == ALIGN
     assert qu(c=A[0] + 16) == ALIAS and qu(s=A[1] + 16) == ALIAS
 
