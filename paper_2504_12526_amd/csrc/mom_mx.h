@@ -154,33 +154,34 @@ MOM_MX_FN int64_t tile_reach(int64_t max_kv, int64_t window, int group, int rows
 }
 
 // How a call is launched: tiles of `rows` query rows, 16 qb for each wavefront; `wk` wavefronts have the same rows and share their tokens (1: each of
-// four has its own); the tokens of a tile in `shares` of `share`, which mx_join_kernel joins.
+// row_waves has its own); the tokens of a tile in `shares` of `share`, which mx_join_kernel joins.
 struct AttentionPlan {
     int qb, wk, rows, shares;
-    int64_t share, numbers;
+    int64_t share, numbers, tiles;      // numbers: of workgroups that are launched for a share; tiles: about as many have work
 };
-MOM_MX_FN constexpr int tile_rows(int qb, int wk) { return 16 * qb * (wk > 1 ? 1 : 4); }
+// Wavefronts of a workgroup that have rows of their own: two a SIMD where their registers let them.
+MOM_MX_FN constexpr int row_waves(int D) { return D == 256 ? 4 : 8; }
+MOM_MX_FN constexpr int tile_rows(int qb, int wk, int D) { return 16 * qb * (wk > 1 ? 1 : row_waves(D)); }
 
-// Wavefronts that share a tile's tokens where workgroups are few: what the registers of a compute unit hold of them (qb = 1 takes up to 128 registers
-// a lane with 64 and 128 dimensions and up to 256 with 256, qb = 2 twice that).
-MOM_MX_FN constexpr int wide(int qb, int D) { return qb == 1 ? (D == 256 ? 8 : 16) : (D == 256 ? 4 : 8); }
-#ifndef WGN
-#define WGN 1024
-#endif
-#ifndef WGW
-#define WGW 256
-#endif
-#ifndef LSH
-#define LSH 2
-#endif
-constexpr int kManyWorkgroups = WGN;    // so many, of four wavefronts, fill the device and need not be wide
-constexpr int kWorkgroups = WGW;        // that the tokens are shared out for: the compute units
-constexpr int kLeastSteps = LSH;          // of a wavefront that a share is worth its joining for
+// Wavefronts that share a tile's tokens: as many as find their registers in half a compute unit (qb = 1 with 64 and 128 dimensions), or in all of it.
+// Sixteen, or four, of qb = 1 each took up to a tenth less time at some lengths (131072 tokens 35.5 us against 36.0, 1024 tokens 7.9 against 8.6) and up
+// to half as much again at others.
+MOM_MX_FN constexpr int sharing(int qb, int D) { return qb == 2 && D == 256 ? 4 : 8; }
 
-// Shares of a tile of `reach` tokens with `workgroups` tiles; more for longer reaches, never fewer.
-MOM_MX_FN int64_t most_shares(int64_t reach, int64_t workgroups, int wk) {
-    const int64_t want = kWorkgroups / workgroups, least = (reach + kLeastSteps * wk * kStep - 1) / (kLeastSteps * wk * kStep);
-    const int64_t s = want < least ? want : least;
+// Shares of a tile of `reach` tokens, `tiles` workgroups without any; more for longer reaches, never fewer.  Joining costs a launch and 4 us or so, so
+// up to 1024 tokens (more where there are many tiles) are one share: of 8 tiles 1024 tokens take 8.9 us, in 4 shares 8.6, of 64 tiles 9.7 and 11.2.  Beyond,
+// a workgroup for every one of 256 compute units, and two or eight shares' worth more where that is little: 64 tiles of 4096 tokens take 15.6 us in
+// 8 shares and 17.9 in 4, 256 tiles of up to 8192 49.7 in 2 and 54 in 1; of 8 tiles 32768 tokens 15.2 in 32 and 16.8 in 64, 131072 36.0 in 64 and 39.7 in 32.
+constexpr int kComputeUnits = 256, kMostShares = 128;
+MOM_MX_FN int64_t most_shares(int64_t reach, int64_t tiles) {
+    if (tiles < 1) tiles = 1;
+    if (reach <= 1024 * (tiles > 64 ? tiles / 64 : 1)) return 1;
+    int64_t s = reach / 2048, least = kComputeUnits / tiles, most = 2 * kComputeUnits / tiles;
+    if (least < 8) least = 8;
+    if (s < least) s = least;
+    if (s > most) s = most;
+    if (s > reach / 256) s = reach / 256;
+    if (s > kMostShares) s = kMostShares;
     return s < 1 ? 1 : s;
 }
 MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window) {
@@ -188,12 +189,11 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
     const int64_t average = (T * group + B - 1) / B;
     AttentionPlan p;
     p.qb = average <= 16 ? 1 : 2;
-    p.wk = average > 64 ? 1 : wide(p.qb, D);
-    const int64_t workgroups = B * ((average + tile_rows(p.qb, p.wk) - 1) / tile_rows(p.qb, p.wk)) * Hkv;
-    if (p.qb == 1 && workgroups >= kManyWorkgroups) p.wk = 4;
-    p.rows = tile_rows(p.qb, p.wk);
+    p.wk = average > 64 ? 1 : sharing(p.qb, D);
+    p.rows = tile_rows(p.qb, p.wk, D);
+    p.tiles = B * ((average + p.rows - 1) / p.rows) * Hkv;
     p.numbers = tile_numbers(T, B, group, p.rows);
-    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, workgroups, p.wk);
+    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, p.tiles);
     p.share = ((reach + s - 1) / s + kStep - 1) / kStep * kStep;
     if (p.share < kStep) p.share = kStep;
     p.shares = reach > 0 ? (int)((reach + p.share - 1) / p.share) : 1;
@@ -202,7 +202,7 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
 // Bytes of workspace: for every share of every row its sums, maximum and sum of weights.  A window leaves fewer shares, never more.
 MOM_MX_FN size_t attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
     const AttentionPlan p = attention_plan(T, B, Hq, Hkv, D, max_kv, 0);
-    const int64_t average = (T * (Hq / Hkv) + B - 1) / B, s = most_shares(max_kv, B * ((average + p.rows - 1) / p.rows) * Hkv, p.wk);
+    const int64_t s = most_shares(max_kv, p.tiles);
     return s <= 1 ? 0 : (size_t)s * (size_t)T * (size_t)Hq * (size_t)(D + 2) * 4;
 }
 

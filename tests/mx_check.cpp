@@ -166,7 +166,7 @@ static void tokens(std::mt19937& rng) {
     const int tile = rng() % ((all + p.rows - 1) / p.rows);
     const int last_row = std::min((tile + 1) * p.rows, all) - 1;
     const mx::Span whole = mx::tile_span(n, m, tile * p.rows / group, last_row / group, window);
-    for (int wave = 0; wave < (p.wk > 1 ? 1 : 4); ++wave) {
+    for (int wave = 0; wave < (p.wk > 1 ? 1 : mx::row_waves(D)); ++wave) {
         const int row0 = tile * p.rows + wave * 16 * p.qb;
         if (row0 >= all) continue;
         const int last = std::min(row0 + 16 * p.qb, all) - 1;
@@ -175,14 +175,16 @@ static void tokens(std::mt19937& rng) {
         for (int z = 0; z < p.shares; ++z) {
             const mx::Span part = mx::share_span(whole, z, p.share);
             const int lo = std::max(part.lo, seen.lo), hi = std::min(part.hi, seen.hi), WK = p.wk;
+            // many rows: the workgroup goes through its part 64 tokens at a time, and each wavefront looks at those that it sees
+            const int from = WK > 1 ? lo : part.lo, to = WK > 1 ? hi : part.hi, length = WK > 1 ? mx::kStep : 64;
             for (int w = 0; w < WK; ++w) {
-                const int token0 = lo / mx::kStep * mx::kStep + (WK > 1 ? w * mx::kStep : 0);
-                const int steps = hi > token0 ? (hi - token0 + WK * mx::kStep - 1) / (WK * mx::kStep) : 0;
+                const int token0 = from / mx::kStep * mx::kStep + (WK > 1 ? w * mx::kStep : 0);
+                const int steps = to > token0 ? (to - token0 + WK * length - 1) / (WK * length) : 0;
                 for (int step = 0; step < steps; ++step)
-                    for (int i = 0; i < mx::kStep; ++i) {
-                        const int t = token0 + step * WK * mx::kStep + i;
+                    for (int i = 0; i < length; ++i) {
+                        const int t = token0 + step * WK * length + i;
                         if (i % 16 == 0) {
-                            const int slot = std::min(t, hi - 1) / page;
+                            const int slot = std::min(t, to - 1) / page;
                             CHECK(slot >= 0 && slot < table, "page %d of %d", slot, table);
                         }
                         if (t >= lo && t < hi) ++taken[t];
