@@ -154,14 +154,15 @@ MOM_MX_FN int64_t tile_reach(int64_t max_kv, int64_t window, int group, int rows
 }
 
 // How a call is launched: tiles of `rows` query rows, 16 qb for each wavefront; `wk` wavefronts have the same rows and share their tokens (1: each of
-// row_waves has its own); the tokens of a tile in `shares` of `share`, which mx_join_kernel joins.
+// kRowWaves has its own); the tokens of a tile in `shares` of `share`, which mx_join_kernel joins.
 struct AttentionPlan {
     int qb, wk, rows, shares;
     int64_t share, numbers, tiles;      // numbers: of workgroups that are launched for a share; tiles: about as many have work
 };
-// Wavefronts of a workgroup that have rows of their own: two a SIMD where their registers let them.
-MOM_MX_FN constexpr int row_waves(int D) { return D == 256 ? 4 : 8; }
-MOM_MX_FN constexpr int tile_rows(int qb, int wk, int D) { return 16 * qb * (wk > 1 ? 1 : row_waves(D)); }
+// Wavefronts of a workgroup that have rows of their own, two a SIMD, and their blocks of 16: what their registers let them.
+constexpr int kRowWaves = 8;
+MOM_MX_FN constexpr int row_blocks(int D) { return D == 256 ? 1 : 2; }
+MOM_MX_FN constexpr int tile_rows(int qb, int wk) { return 16 * qb * (wk > 1 ? 1 : kRowWaves); }
 
 // Wavefronts that share a tile's tokens: as many as find their registers in half a compute unit (qb = 1 with 64 and 128 dimensions), or in all of it.
 // Sixteen, or four, of qb = 1 each took up to a tenth less time at some lengths (131072 tokens 35.5 us against 36.0, 1024 tokens 7.9 against 8.6) and up
@@ -188,9 +189,9 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
     const int group = Hq / Hkv;
     const int64_t average = (T * group + B - 1) / B;
     AttentionPlan p;
-    p.qb = average <= 16 ? 1 : 2;
-    p.wk = average > 64 ? 1 : sharing(p.qb, D);
-    p.rows = tile_rows(p.qb, p.wk, D);
+    p.wk = average > 64 ? 1 : sharing(average <= 16 ? 1 : 2, D);
+    p.qb = average <= 16 ? 1 : p.wk == 1 ? row_blocks(D) : 2;
+    p.rows = tile_rows(p.qb, p.wk);
     p.tiles = B * ((average + p.rows - 1) / p.rows) * Hkv;
     p.numbers = tile_numbers(T, B, group, p.rows);
     const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, p.tiles);

@@ -166,7 +166,7 @@ static void tokens(std::mt19937& rng) {
     const int tile = rng() % ((all + p.rows - 1) / p.rows);
     const int last_row = std::min((tile + 1) * p.rows, all) - 1;
     const mx::Span whole = mx::tile_span(n, m, tile * p.rows / group, last_row / group, window);
-    for (int wave = 0; wave < (p.wk > 1 ? 1 : mx::row_waves(D)); ++wave) {
+    for (int wave = 0; wave < (p.wk > 1 ? 1 : mx::kRowWaves); ++wave) {
         const int row0 = tile * p.rows + wave * 16 * p.qb;
         if (row0 >= all) continue;
         const int last = std::min(row0 + 16 * p.qb, all) - 1;
