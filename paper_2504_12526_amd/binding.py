@@ -109,13 +109,15 @@ def status_string(status):
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
+    """Handle of a stream, None: the current one of the current device (asked by its number: a torch Stream object takes 4 us to make, which is
+    more than a small kernel)."""
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _nbytes(t):
@@ -283,7 +285,7 @@ def mom_kv_reload(pinned_host, k, v, stream, done_event=None, check=True):
 
 
 def _dense(name, t, dtype, shape=None):
-    if t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dtype != dtype or (shape is not None and t.shape != shape) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor" + ("" if shape is None else f" of shape {tuple(shape)}"))
     return t
 
@@ -291,20 +293,27 @@ def _dense(name, t, dtype, shape=None):
 def _tokens(name, t, width=None):
     """[T, heads, head_dim] bf16 whose tokens may lie apart; the elements between two of them."""
     T, heads, d = t.shape
-    if t.dtype != torch.bfloat16 or (heads > 1 and t.stride(1) != d) or t.stride(2) != 1 or (width is not None and (T, d) != width):
+    apart, between, within = t.stride()
+    if t.dtype != torch.bfloat16 or (heads > 1 and between != d) or within != 1 or (width is not None and (T, d) != width):
         raise ValueError(f"{name} must be a bfloat16 tensor [tokens, heads, head_dim] whose heads are contiguous")
-    return t.stride(0) if T > 1 else heads * d
+    return apart if T > 1 else heads * d
+
+
+_block_bytes = {}
+
+
+def mom_mx_block_bytes(head_dim, page_tokens):
+    n = _block_bytes.get((head_dim, page_tokens))
+    if n is None:
+        n = _block_bytes[head_dim, page_tokens] = int(lib().mom_mx_block_bytes(int(head_dim), int(page_tokens)))
+    return n
 
 
 def _cache(cache, page_tokens, head_dim):
     block = mom_mx_block_bytes(head_dim, page_tokens)
-    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or block == 0 or cache.shape[2] != block:
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or block == 0 or cache.shape[2] != block or not cache.is_contiguous():
         raise ValueError("cache must be a contiguous uint8 tensor [pages, kv_heads, mom_mx_block_bytes(head_dim, page_tokens)]")
     return cache.shape[0], cache.shape[1]
-
-
-def mom_mx_block_bytes(head_dim, page_tokens):
-    return int(lib().mom_mx_block_bytes(int(head_dim), int(page_tokens)))
 
 
 def mom_mx_kv_append(k, v, slots, cache, page_tokens, positions=None, inv_freq=None, interleaved=False, q=None, q_out=None,
@@ -314,7 +323,7 @@ def mom_mx_kv_append(k, v, slots, cache, page_tokens, positions=None, inv_freq=N
     and, where given, the queries q [T, q_heads, head_dim] into q_out."""
     T, kv_heads, d = k.shape
     pages, heads = _cache(cache, page_tokens, d)
-    if tuple(v.shape) != tuple(k.shape) or heads != kv_heads:
+    if v.shape != k.shape or heads != kv_heads:
         raise ValueError("k and v must have the same shape and the cache their heads")
     if (positions is None) != (inv_freq is None) or (q is None) != (q_out is None):
         raise ValueError("positions and inv_freq, q and q_out come together")

@@ -4,7 +4,8 @@
 //
 // A code is sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; a scale byte b stands for 2^(b - 127),
 // 255 for NaN.  gfx950 turns two codes and a scale into two bf16 numbers in one instruction, exactly (8 significant bits hold every product), so
-// nothing is rounded between the cache and the matrix cores.
+// nothing is rounded between the cache and the matrix cores; and two numbers and a scale into two codes: the nearest, ties to the even one, above 6 the
+// largest.
 #ifndef MOM_MX_H
 #define MOM_MX_H
 
@@ -27,55 +28,34 @@ constexpr int kMinExponent = -125, kMaxExponent = 125;  // of a scale that the l
 
 // ---- encoding -------------------------------------------------------------------------------------------------------------
 
-// What encodes a number: its magnitude as bits (which order like the magnitudes, infinities and NaN last) and the parts of them.
-struct F32 {
-    typedef float value;
-    typedef uint32_t bits;
-    static constexpr int kMantissa = 23, kBias = 127;
-};
-struct F64 {
-    typedef double value;
-    typedef uint64_t bits;
-    static constexpr int kMantissa = 52, kBias = 1023;
-};
-
-template <class F>
-MOM_MX_FN typename F::bits magnitude_bits(typename F::value x) {
-    typename F::bits b;
-    memcpy(&b, &x, sizeof b);
-    return b << 1 >> 1;
+// The bits of a magnitude, which order like it, infinities and NaN last.
+MOM_MX_FN uint32_t magnitude(float x) {
+    uint32_t b;
+    memcpy(&b, &x, 4);
+    return b & 0x7fffffffu;
 }
-template <class F>
-MOM_MX_FN bool finite(typename F::bits magnitude) {
-    return (magnitude >> F::kMantissa) < (typename F::bits)(2 * F::kBias + 1);
-}
+MOM_MX_FN bool finite(uint32_t magnitude) { return magnitude < 0x7f800000u; }
 
 // Exponent of the scale of a block whose largest magnitude is `top` (finite): the power of two that brings it to at most 7, which is half a step
 // away from the largest element 6, so that no element is further than half a step from its code (the rounding down to [4, 8) that is
 // also in use cuts off up to a quarter of the largest element).
-template <class F>
-MOM_MX_FN int scale_exponent(typename F::bits top) {
-    const typename F::bits fraction = top & (((typename F::bits)1 << F::kMantissa) - 1);
-    const int e = (int)(top >> F::kMantissa) - F::kBias - 2 + (fraction > ((typename F::bits)3 << (F::kMantissa - 2)) ? 1 : 0);
+MOM_MX_FN int scale_exponent(uint32_t top) {
+    const int e = (int)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > (3u << 21) ? 1 : 0);
     return e < kMinExponent ? kMinExponent : e > kMaxExponent ? kMaxExponent : e;
 }
 
-// 2^-e for the exponent of a scale.
-template <class F>
-MOM_MX_FN typename F::value inverse_scale(int e) {
-    const typename F::bits b = (typename F::bits)(F::kBias - e) << F::kMantissa;
-    typename F::value v;
-    memcpy(&v, &b, sizeof v);
-    return v;
-}
-
-// The code of x, `inverse` from inverse_scale: the nearest element, ties to the even code, above 6 the largest.
-template <class F>
-MOM_MX_FN uint32_t encode(typename F::value x, typename F::value inverse) {
-    typedef typename F::value V;
-    const V a = (x < 0 ? -x : x) * inverse;             // exact: a power of two
-    return (uint32_t)(a > (V)0.25) + (uint32_t)(a >= (V)0.75) + (uint32_t)(a > (V)1.25) + (uint32_t)(a >= (V)1.75) + (uint32_t)(a > (V)2.5) +
-           (uint32_t)(a >= (V)3.5) + (uint32_t)(a > (V)5.0) + (x < 0 ? 8u : 0u);
+// x in 32 bits, cut off, the last bit set if anything was: on the same side of every number of fewer bits, borders between codes among them, as x (a
+// rounded one may come to lie on a border, whose ties then go the wrong way).
+MOM_MX_FN float cut_to_odd(double x) {
+    const float f = (float)x;
+    const double back = (double)f;
+    uint32_t b;
+    memcpy(&b, &f, 4);
+    if ((back < 0 ? -back : back) > (x < 0 ? -x : x)) b -= 1;
+    if (back != x) b |= 1;
+    float r;
+    memcpy(&r, &b, 4);
+    return r;
 }
 
 // ---- layout of the paged cache --------------------------------------------------------------------------------------------

@@ -1,6 +1,6 @@
 // Host-side check of what the four-bit kernels (csrc/mom_mx_*.hip.inc) take from csrc/mom_mx.h:
 //   1. a cache block's bytes: what the tokens append fills it, every nibble once, and what attention loads lies inside it;
-//   2. codes are the nearest elements, ties to even, scales the smallest that leave at most 7;
+//   2. scales are the smallest that leave at most 7, and a number that is cut to 32 bits goes to the code of the whole one;
 //   3. tile numbers: every tile of every sequence has one of its own, all under the number of them;
 //   4. tokens: the steps of the wavefronts over all shares take every token that a tile sees once, pages are looked up inside the table,
 //      and the workspace holds the shares of every window.
@@ -66,43 +66,47 @@ static void layout(int P, int D) {
         }
 }
 
-template <class F>
-static void encoding(std::mt19937& rng) {
-    typedef typename F::value V;
+// The code of a magnitude in units of the scale, by the definition.
+static int code_of(double a) {
     const double mags[8] = {0, 0.5, 1, 1.5, 2, 3, 4, 6};
+    int best = 0;
+    for (int k = 1; k < 8; ++k) {
+        const double o = std::fabs(a - mags[k]), b = std::fabs(a - mags[best]);
+        if (o < b || (o == b && k % 2 == 0)) best = k;
+    }
+    return best;
+}
+
+static void encoding(std::mt19937& rng) {
     std::normal_distribution<double> normal(0, 1);
     for (int i = 0; i < 20000; ++i) {
-        V x[32], top = 0;
-        const int mode = i % 5, e = (int)(rng() % 200) - 100;
-        for (V& v : x) {
-            const double m = mode == 0 ? normal(rng) : mode == 1 ? (double)(int)(rng() % 57) / 8 : mode == 2 ? (double)(int)(rng() % 29) / 4 : mode == 3 ? 0.0 : 7 * (rng() % 2);
-            v = (V)std::ldexp(rng() % 2 ? m : -m, mode == 0 ? 0 : e);
-            top = std::fabs(v) > top ? std::fabs(v) : top;
+        double x[32], top = 0;
+        uint32_t bits = 0;
+        const int mode = i % 5, e = i % 7 == 0 ? (int)(rng() % 24) - 140 : (int)(rng() % 200) - 100;
+        for (double& v : x) {
+            double m = mode == 0 ? normal(rng) : mode == 1 ? (double)(int)(rng() % 57) / 8 : mode == 2 ? (double)(int)(rng() % 29) / 4 : mode == 3 ? 0.0 : 7 * (rng() % 2);
+            if (rng() % 8 == 0) m = std::nextafter(m, rng() % 2 ? 8.0 : 0.0);        // right beside a border
+            v = std::ldexp(rng() % 2 ? m : -m, mode == 0 ? 0 : e);
+            const float f = mx::cut_to_odd(v);
+            CHECK(std::signbit(f) == std::signbit(v), "sign of %g", v);
+            bits = std::max(bits, mx::magnitude(f));
+            top = std::max(top, std::fabs(v));
         }
-        typename F::bits bits = 0;
-        for (V v : x) bits = std::max(bits, mx::magnitude_bits<F>(v));
-        CHECK(mx::finite<F>(bits), "finite");
-        const int s = mx::scale_exponent<F>(bits);
+        CHECK(mx::finite(bits), "finite");
+        const int s = mx::scale_exponent(bits);
         if (top > 0) {
-            CHECK(top <= std::ldexp(7.0, s), "top %g at scale %d", (double)top, s);
-            CHECK(top > std::ldexp(7.0, s - 1), "scale %d is not the smallest of %g", s, (double)top);
+            CHECK(top <= std::ldexp(7.0, s), "top %g at scale %d", top, s);
+            CHECK(s == mx::kMinExponent || top > std::ldexp(7.0, s - 1), "scale %d is not the smallest of %g", s, top);
         }
-        const V inverse = mx::inverse_scale<F>(s);
-        CHECK((double)inverse == std::ldexp(1.0, -s), "inverse of %d", s);
-        for (V v : x) {
-            const unsigned c = mx::encode<F>(v, inverse);
-            const double a = std::fabs(std::ldexp((double)v, -s)), off = std::fabs(a - mags[c & 7]);
-            CHECK((c >> 3) == (v < 0), "sign of %g", (double)v);
-            for (int k = 0; k < 8; ++k) {
-                const double o = std::fabs(a - mags[k]);
-                CHECK(o > off || (o == off && (k == (int)(c & 7) || !(c & 1))), "%g is code %u, %d is nearer", a, c, k);
-            }
+        for (double v : x) {
+            const double a = std::fabs(std::ldexp(v, -s)), b = std::fabs(std::ldexp((double)mx::cut_to_odd(v), -s));
+            CHECK(code_of(a) == code_of(b), "%.17g goes to code %d, in 32 bits to %d", a, code_of(a), code_of(b));
         }
     }
-    for (double v : {(double)INFINITY, -(double)INFINITY, (double)NAN}) CHECK(!mx::finite<F>(mx::magnitude_bits<F>((V)v)), "%g is finite", v);
-    CHECK(mx::scale_exponent<F>(0) == mx::kMinExponent, "scale of nothing");
-    CHECK(mx::scale_exponent<F>(mx::magnitude_bits<F>((V)std::numeric_limits<float>::max())) == mx::kMaxExponent, "largest scale");
-    CHECK((mx::encode<F>((V)std::numeric_limits<float>::max(), mx::inverse_scale<F>(mx::kMaxExponent)) & 7) == 7, "largest code");
+    for (double v : {(double)INFINITY, -(double)INFINITY, (double)NAN}) CHECK(!mx::finite(mx::magnitude(mx::cut_to_odd(v))), "%g is finite", v);
+    CHECK(mx::finite(mx::magnitude(mx::cut_to_odd(4e38))), "more than 32 bits hold is finite");
+    CHECK(mx::scale_exponent(0) == mx::kMinExponent, "scale of nothing");
+    CHECK(mx::scale_exponent(mx::magnitude(std::numeric_limits<float>::max())) == mx::kMaxExponent, "largest scale");
 }
 
 static void numbers(std::mt19937& rng) {
@@ -211,8 +215,7 @@ int main() {
         }
     for (int P : {-16, 0, 8, 24, 48, 512}) CHECK(!mx::page_served(P), "page of %d", P);
     std::mt19937 rng(7);
-    encoding<mx::F32>(rng);
-    encoding<mx::F64>(rng);
+    encoding(rng);
     for (uint32_t group = 1; group < (1 << 15); group += group < 300 ? 1 : 977)
         for (uint32_t r = 0; r < (1 << 16) + (1 << 15); r += r < 2000 ? 1 : 313)
             CHECK(mx::divided(r, mx::inverse_of(group)) == r / group, "divided: %u / %u", r, group);

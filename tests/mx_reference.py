@@ -24,7 +24,7 @@ def encode(x):
     tie = off == low
     # of two tied neighbours one is even
     code = torch.where(tie, torch.tensor([2, 1, 2, 1, 2, 1, 2, 1]), 0).argmax(-1)
-    code = code + 8 * (b < 0).long()
+    code = code + 8 * torch.signbit(b).long()
     code = torch.where(fine.unsqueeze(-1), code, 0)
     return code.flatten(-2), torch.where(fine, e + 127, 255)
 

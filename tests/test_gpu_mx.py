@@ -140,6 +140,21 @@ def test_append_rotates_dense_queries_in_place():
     assert torch.equal(gq.view(torch.int16), q_out.view(torch.int16))
 
 
+def test_append_rotates_infinities_and_nan():
+    """An infinity stays one, opposite ones and NaN are NaN, in the two dimensions that they turn into and nowhere else."""
+    T, D, P = 4, 64, 16
+    gen = _gen(6)
+    q, k = _normal(gen, T, 1, D), _normal(gen, T, 1, D)
+    q[0, 0, 3], q[1, 0, 40], q[2, 0, 5], q[3, 0, 7], q[3, 0, 39] = math.inf, -math.inf, math.nan, math.inf, math.inf
+    positions, inv_freq = torch.tensor([1, 5, 9, 100], dtype=torch.int32), (10000.0 ** (-torch.arange(0, D, 2).double() / D)).float()
+    q_out = torch.empty_like(q, device=DEV)
+    binding.mom_mx_kv_append(k.to(DEV), k.to(DEV), torch.arange(T).to(DEV), torch.zeros(1, 1, ref.block_bytes(P, D), dtype=torch.uint8, device=DEV), P,
+                             positions=positions.to(DEV), inv_freq=inv_freq.to(DEV), q=q.to(DEV), q_out=q_out)
+    want = ref.rotate(q, positions, inv_freq, False)
+    assert torch.isinf(want[:2]).sum() == 4 and torch.isnan(want).sum() >= 2
+    _within(q_out, want, want.abs() * (ref.BF16_HALF + 2 * ref.F32_HALF) + 1e-14)
+
+
 # Attention
 
 def _sequences(gen, Hkv, D, P, lens, extra=3, values=1.0):

@@ -32,9 +32,10 @@ def test_layout_encoding_tiles_and_shares(tmp_path):
 @pytest.mark.parametrize("old,new,says", [
     ("P * (D / 2 + D / 32) + quad * 2 * D", "P * (D / 2 + D / 32) + quad * D", "filled"),
     ("P * (D + D / 32) + quad * (D / 8)", "P * (D + D / 16) + quad * (D / 8)", "append"),
-    ("(a >= (V)1.75)", "(a > (V)1.75)", "nearer"),
-    ("(uint32_t)(a > (V)2.5)", "(uint32_t)(a >= (V)2.5)", "nearer"),
-    ("kBias - 2 + (fraction", "kBias - 3 + (fraction", "scale"),
+    ("if (back != x) b |= 1;", "", "code"),
+    ("b -= 1;", "b -= 0;", "code"),
+    ("- 127 - 2 + ((top", "- 127 - 3 + ((top", "scale"),
+    ("> (3u << 21) ? 1 : 0", ">= (3u << 21) ? 1 : 0", "scale"),
     ("{ return start * group / rows + b; }", "{ return start * group / rows; }", "number"),
     ("if (b >= B || tile < 0", "if (tile < 0", "sequence"),
     ("(uint32_t)tile >= (m * group + rows - 1) / rows)", "(uint32_t)tile > (m * group + rows - 1) / rows)", "number"),
