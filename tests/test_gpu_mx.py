@@ -362,7 +362,7 @@ def _weight(gen, N, K, std=0.05):
     return ref.pack(codes), scales.to(torch.uint8)
 
 
-@pytest.mark.parametrize("N,K", [(1, 32), (16, 64), (17, 96), (33, 128), (50, 160), (300, 1056), (129, 2080), (64, 4096), (2049 * 16 + 5, 64), (40, 14336)])
+@pytest.mark.parametrize("N,K", [(1, 32), (16, 64), (17, 96), (33, 128), (50, 160), (300, 1056), (129, 2080), (64, 4096), (2049 * 16 + 5, 64), (40, 14336), (33, 32768), (32800, 2208), (20, 8224)])
 @pytest.mark.parametrize("M", [1, 2, 5, 16])
 def test_products(N, K, M):
     gen = _gen(30)
