@@ -148,6 +148,10 @@ MOM_MX_FN constexpr int tile_rows(int qb, int wk) { return 16 * qb * (wk > 1 ? 1
 // Sixteen, or four, of qb = 1 each took up to a tenth less time at some lengths (131072 tokens 35.5 us against 36.0, 1024 tokens 7.9 against 8.6) and up
 // to half as much again at others.
 MOM_MX_FN constexpr int sharing(int qb, int D) { return qb == 2 && D == 256 ? 4 : 8; }
+// Of qb = 1 with fewer than 256 dimensions four where there are so many tiles that each compute unit has several anyway, and few steps for each wavefront:
+// 128 sequences of up to 512 tokens and 8 key heads 15.8 us, 20.1 with eight; of up to 2048 tokens 42.2 and 45.1; 96 sequences of 512 14.7 and 17.5.  Eight
+// are ahead with fewer tiles (64 sequences of 512 11.9 us, 12.3 with four), longer reaches (128 of 8192 142 and 149) and 256 dimensions (95 and 102).
+constexpr int kNarrow = 4, kManyTiles = 768, kNarrowReach = 2048;
 
 // Shares of a tile of `reach` tokens, `tiles` workgroups without any; more for longer reaches, never fewer.  Joining costs a launch and 4 us or so, so
 // up to 1024 tokens (more where there are many tiles) are one share: of 8 tiles 1024 tokens take 8.9 us, in 4 shares 8.6, of 64 tiles 9.7 and 11.2.  Beyond,
@@ -175,6 +179,7 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
     p.tiles = B * ((average + p.rows - 1) / p.rows) * Hkv;
     p.numbers = tile_numbers(T, B, group, p.rows);
     const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, p.tiles);
+    if (p.qb == 1 && D < 256 && p.tiles >= kManyTiles && reach <= kNarrowReach) p.wk = kNarrow;
     p.share = ((reach + s - 1) / s + kStep - 1) / kStep * kStep;
     if (p.share < kStep) p.share = kStep;
     p.shares = reach > 0 ? (int)((reach + p.share - 1) / p.share) : 1;

@@ -225,6 +225,13 @@ def test_long_sequences_are_shared_out(Hq, Hkv, D, P, lens, asked, window):
     _compare(_gen(14), Hq, Hkv, D, P, lens, asked, window)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 8, 64), (8, 8, 128), (8, 4, 256)])
+def test_many_short_sequences(Hq, Hkv, D):
+    """More tiles than 768: a workgroup has four wavefronts, with 256 dimensions eight."""
+    B = 1100 // Hkv
+    _compare(_gen(25), Hq, Hkv, D, 16, [1 + (7 * b) % 45 for b in range(B)], [1] * B)
+
+
 def test_rows_that_see_nothing():
     gen = _gen(15)
     # no tokens at all; fewer in the cache than asked about (the first stand before the beginning); lengths that are none
