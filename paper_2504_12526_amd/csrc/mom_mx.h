@@ -145,27 +145,31 @@ MOM_MX_FN constexpr int row_blocks(int D) { return D == 256 ? 1 : 2; }
 MOM_MX_FN constexpr int tile_rows(int qb, int wk) { return 16 * qb * (wk > 1 ? 1 : kRowWaves); }
 
 // Wavefronts that share a tile's tokens: as many as find their registers in half a compute unit (qb = 1 with 64 and 128 dimensions), or in all of it.
-// Sixteen, or four, of qb = 1 each took up to a tenth less time at some lengths (131072 tokens 35.5 us against 36.0, 1024 tokens 7.9 against 8.6) and up
-// to half as much again at others.
+// Of qb = 1 four and sixteen each took longer: one sequence of 1024 tokens 9.0 us, 9.7 with four and 10.1 with sixteen, of 131072 37.2, 39.5 and 43.3, 32
+// sequences of up to 8192 47.0, 63.0 and 54.1.
 MOM_MX_FN constexpr int sharing(int qb, int D) { return qb == 2 && D == 256 ? 4 : 8; }
 // Of qb = 1 with fewer than 256 dimensions four where there are so many tiles that each compute unit has several anyway, and few steps for each wavefront:
 // 128 sequences of up to 512 tokens and 8 key heads 15.8 us, 20.1 with eight; of up to 2048 tokens 42.2 and 45.1; 96 sequences of 512 14.7 and 17.5.  Eight
 // are ahead with fewer tiles (64 sequences of 512 11.9 us, 12.3 with four), longer reaches (128 of 8192 142 and 149) and 256 dimensions (95 and 102).
 constexpr int kNarrow = 4, kManyTiles = 768, kNarrowReach = 2048;
 
-// Shares of a tile of `reach` tokens, `tiles` workgroups without any; more for longer reaches, never fewer.  Joining costs a launch and 4 us or so, so
-// up to 1024 tokens (more where there are many tiles) are one share: of 8 tiles 1024 tokens take 8.9 us, in 4 shares 8.6, of 64 tiles 9.7 and 11.2.  Beyond,
-// a workgroup for every one of 256 compute units, and two or eight shares' worth more where that is little: 64 tiles of 4096 tokens take 15.6 us in
-// 8 shares and 17.9 in 4, 256 tiles of up to 8192 49.7 in 2 and 54 in 1; of 8 tiles 32768 tokens 15.2 in 32 and 16.8 in 64, 131072 36.0 in 64 and 39.7 in 32.
-constexpr int kComputeUnits = 256, kMostShares = 128;
+// Shares of a tile of `reach` tokens, `tiles` workgroups without any; more for longer reaches, never fewer.  Joining costs a launch, so short reaches are
+// one share: up to 768 tokens of up to 16 tiles (of 8 tiles 512 tokens take 6.8 us, 7.7 in 4 shares; 1024 tokens 9.0, and 8.0 in 8), and up to 1024, or more
+// where there are many tiles, of others (64 tiles 9.5 us, 11.0 in 4).  Beyond, a workgroup for every one of 256 compute units, and two or eight shares' worth
+// more where that is little: 64 tiles of 4096 tokens take 15.0 us in 8 shares and 17.4 in 4, 256 tiles of up to 8192 47.2 in 2 and 61.8 in 1; of 8 tiles
+// 32768 tokens 15.5 in 32 and 17.1 in 64, 131072 37.1 in 64 and 40.9 in 32.  A share has 256 tokens, of few tiles' short reaches 128 (2048 tokens 8.4 us
+// in 16 shares, 8.8 in 8).
+constexpr int kComputeUnits = 256, kMostShares = 128, kFewTiles = 16;
 MOM_MX_FN int64_t most_shares(int64_t reach, int64_t tiles) {
     if (tiles < 1) tiles = 1;
-    if (reach <= 1024 * (tiles > 64 ? tiles / 64 : 1)) return 1;
+    if (reach <= (tiles <= kFewTiles ? 768 : 1024 * (tiles > 64 ? tiles / 64 : 1))) return 1;
     int64_t s = reach / 2048, least = kComputeUnits / tiles, most = 2 * kComputeUnits / tiles;
     if (least < 8) least = 8;
     if (s < least) s = least;
     if (s > most) s = most;
-    if (s > reach / 256) s = reach / 256;
+    int64_t whole = reach / 256;
+    if (tiles <= kFewTiles && whole < 16) whole = reach / 128 < 16 ? reach / 128 : 16;
+    if (s > whole) s = whole;
     if (s > kMostShares) s = kMostShares;
     return s < 1 ? 1 : s;
 }
