@@ -78,26 +78,27 @@ MOM_MX_FN bool page_served(int64_t P) { return P >= 16 && P <= 256 && (P & (P - 
 
 // ---- tiles of attention ---------------------------------------------------------------------------------------------------
 
-// The query rows of a sequence at one key head, `group` query heads for each of its tokens, are cut into tiles of `rows`.  Where the tokens of a
-// sequence start is known on the device only, so tiles are numbered such that the number of sequence b's first one needs nothing but
-// its start: floor(start * group / rows) + b leaves each at least as many numbers as it has tiles.
+// The query rows of a sequence at one key head, `group` query heads for each of its tokens, are cut into tiles of `rows`, numbered sequence by sequence.
+// Where the tokens of a sequence start is known on the device only, and with it how many tiles there are: at most tile_numbers, those that are none's last
+// (numbers that are none's between the others leave part of the compute units without work, as workgroups are handed out in order: 4 sequences of 8 tokens
+// and 8192 in the cache, 32 rows a tile, took 29.5 us where every second number was none's).
 // (32 bits hold all of it: up to 2^29 tokens and 2^31 rows of queries.)
-MOM_MX_FN uint32_t first_tile(uint32_t start, uint32_t b, uint32_t group, uint32_t rows) { return start * group / rows + b; }
+MOM_MX_FN uint32_t tiles_of(uint32_t m, uint32_t group, uint32_t rows) { return (m * group + rows - 1) / rows; }
 MOM_MX_FN int64_t tile_numbers(int64_t T, int64_t B, int group, int rows) { return T * group / rows + B; }
 
 // The sequence of tile `number`, and which of its tiles it is; b = -1 where the number is no tile's.  Where every sequence has m tokens, and
-// where b is the last whose first number is not behind `number` (0 if there is none).
+// of sequence b whose m tokens have `before` tiles in front of them.
 struct Tile { int b, tile; };
-MOM_MX_FN Tile checked_tile(uint32_t b, int tile, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
-    if (b >= B || tile < 0 || (uint32_t)tile >= (m * group + rows - 1) / rows) return {-1, 0};
-    return {(int)b, tile};
+MOM_MX_FN Tile checked_tile(uint32_t b, uint32_t tile, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
+    if (b >= B || tile >= tiles_of(m, group, rows)) return {-1, 0};
+    return {(int)b, (int)tile};
 }
 MOM_MX_FN Tile even_tile(uint32_t number, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
-    const uint32_t tiles = (m * group + rows - 1) / rows, b = tiles == 1 ? number : number / tiles;
-    return checked_tile(b, (int)(number - b * tiles), B, m, group, rows);
+    const uint32_t tiles = tiles_of(m, group, rows), b = tiles == 1 ? number : number / tiles;
+    return checked_tile(b, number - b * tiles, B, m, group, rows);
 }
-MOM_MX_FN Tile listed_tile(uint32_t number, uint32_t b, uint32_t start, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
-    return checked_tile(b, (int)(number - first_tile(start, b, group, rows)), B, m, group, rows);
+MOM_MX_FN Tile listed_tile(uint32_t number, uint32_t b, uint32_t before, uint32_t B, uint32_t m, uint32_t group, uint32_t rows) {
+    return checked_tile(b, number - before, B, m, group, rows);
 }
 
 // r / group for r < 2^16 + 2^15 and group < 2^15, by a multiplication: inverse = floor(2^32 / group) + 1 is off by less than 1 in 2^32 / group of it.
@@ -137,7 +138,7 @@ MOM_MX_FN int64_t tile_reach(int64_t max_kv, int64_t window, int group, int rows
 // kRowWaves has its own); the tokens of a tile in `shares` of `share`, which mx_join_kernel joins.
 struct AttentionPlan {
     int qb, wk, rows, shares;
-    int64_t share, numbers, tiles;      // numbers: of workgroups that are launched for a share; tiles: about as many have work
+    int64_t share, numbers, tiles;      // numbers: of tiles of a key head at most; tiles: about as many there are, of all heads
 };
 // Wavefronts of a workgroup that have rows of their own, two a SIMD, and their blocks of 16: what their registers let them.
 constexpr int kRowWaves = 8;
@@ -147,13 +148,17 @@ MOM_MX_FN constexpr int tile_rows(int qb, int wk) { return 16 * qb * (wk > 1 ? 1
 // Wavefronts that share a tile's tokens: as many as find their registers in half a compute unit (qb = 1 with 64 and 128 dimensions), or in all of it.
 // Of qb = 1 four and sixteen each took longer: one sequence of 1024 tokens 9.0 us, 9.7 with four and 10.1 with sixteen, of 131072 37.2, 39.5 and 43.3, 32
 // sequences of up to 8192 47.0, 63.0 and 54.1.
-MOM_MX_FN constexpr int sharing(int qb, int D) { return qb == 2 && D == 256 ? 4 : 8; }
+constexpr int kSharing = 8;
+// Rows of a sequence up to which wavefronts share tokens, not rows (one sequence of 210 rows and 40000 tokens 36.0 us, 40.5 with rows of their own; 2 of 80
+// and 9000 21.9 and 28.1), and of them at most 16 a workgroup if there are 256 dimensions (4 sequences of 32 rows and 5000 tokens 17.6 us, 22.1 with 32).
+constexpr int kFewRows = 256;
+MOM_MX_FN constexpr int few_blocks(int D) { return D == 256 ? 1 : 2; }
 // Of qb = 1 with fewer than 256 dimensions four where there are so many tiles that each compute unit has several anyway, and few steps for each wavefront:
 // 128 sequences of up to 512 tokens and 8 key heads 15.8 us, 20.1 with eight; of up to 2048 tokens 42.2 and 45.1; 96 sequences of 512 14.7 and 17.5.  Eight
 // are ahead with fewer tiles (64 sequences of 512 11.9 us, 12.3 with four), longer reaches (128 of 8192 142 and 149) and 256 dimensions (95 and 102).
 constexpr int kNarrow = 4, kManyTiles = 768, kNarrowReach = 2048;
 
-// Shares of a tile of `reach` tokens, `tiles` workgroups without any; more for longer reaches, never fewer.  Joining costs a launch, so short reaches are
+// Shares of a tile of `reach` tokens and qb = 1, `tiles` workgroups without any; more for longer reaches, never fewer.  Joining costs a launch, so short reaches are
 // one share: up to 768 tokens of up to 16 tiles (of 8 tiles 512 tokens take 6.8 us, 7.7 in 4 shares; 1024 tokens 9.0, and 8.0 in 8), and up to 1024, or more
 // where there are many tiles, of others (64 tiles 9.5 us, 11.0 in 4).  Beyond, a workgroup for every one of 256 compute units, and two or eight shares' worth
 // more where that is little: 64 tiles of 4096 tokens take 15.0 us in 8 shares and 17.4 in 4, 256 tiles of up to 8192 47.2 in 2 and 61.8 in 1; of 8 tiles
@@ -173,17 +178,36 @@ MOM_MX_FN int64_t most_shares(int64_t reach, int64_t tiles) {
     if (s > kMostShares) s = kMostShares;
     return s < 1 ? 1 : s;
 }
-MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window) {
+// Shares of the other tiles, of which a compute unit has one at a time: what the rounds of workgroups take, and what a share costs that is stored and
+// joined, as much as 600 tokens' work: the fewest shares of which the sum is smallest, and so no fewer for longer reaches.  It is one whole round where
+// that can be: 2048 tokens against 16384 with 256 tiles 499 us in one share, 540 in two, 562 in four; 512 against 32768 with 64 tiles 267 in four, 279 in
+// eight, 509 in two; 4 sequences of 64 rows and 16384 tokens 35.2 in four, 42.6 in eight.
+constexpr int64_t kShareCost = 600;
+MOM_MX_FN int64_t round_shares(int64_t reach, int64_t tiles) {
+    int64_t best = 1;
+    if (tiles < 1) tiles = 1;
+    const auto cost = [&](int64_t s) {                  // times tiles and s (54 bits)
+        return (tiles * s + kComputeUnits - 1) / kComputeUnits * kComputeUnits * reach + (s > 1 ? kShareCost * s * s * tiles : 0);
+    };
+    for (int64_t s = 2; s <= kMostShares && s <= reach / 256 && tiles * s <= 8 * kComputeUnits; ++s)
+        if (cost(s) * best < cost(best) * s) best = s;
+    return best;
+}
+
+MOM_MX_FN int64_t plan_shares(const AttentionPlan& p, int64_t reach) { return p.wk > 1 && p.qb == 1 ? most_shares(reach, p.tiles) : round_shares(reach, p.tiles); }
+// `listed`: sequences of their own lengths, whose last tiles are half full, say.
+MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window, bool listed) {
     const int group = Hq / Hkv;
     const int64_t average = (T * group + B - 1) / B;
     AttentionPlan p;
-    p.wk = average > 64 ? 1 : sharing(average <= 16 ? 1 : 2, D);
-    p.qb = average <= 16 ? 1 : p.wk == 1 ? row_blocks(D) : 2;
+    p.wk = average > kFewRows ? 1 : kSharing;
+    p.qb = average > kFewRows ? row_blocks(D) : average > 16 ? few_blocks(D) : 1;
     p.rows = tile_rows(p.qb, p.wk);
-    p.tiles = B * ((average + p.rows - 1) / p.rows) * Hkv;
-    p.numbers = tile_numbers(T, B, group, p.rows);
-    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = most_shares(reach, p.tiles);
-    if (p.qb == 1 && D < 256 && p.tiles >= kManyTiles && reach <= kNarrowReach) p.wk = kNarrow;
+    const int64_t even = B * ((average + p.rows - 1) / p.rows), uneven = (2 * T * group + (B + 1) * p.rows - 1) / (2 * p.rows);
+    p.tiles = (!listed ? even : uneven < B ? B : uneven) * Hkv;
+    p.numbers = listed ? tile_numbers(T, B, group, p.rows) : even;
+    const int64_t reach = tile_reach(max_kv, window, group, p.rows), s = plan_shares(p, reach);
+    if (p.wk > 1 && p.qb == 1 && D < 256 && p.tiles >= kManyTiles && reach <= kNarrowReach) p.wk = kNarrow;
     p.share = ((reach + s - 1) / s + kStep - 1) / kStep * kStep;
     if (p.share < kStep) p.share = kStep;
     p.shares = reach > 0 ? (int)((reach + p.share - 1) / p.share) : 1;
@@ -191,8 +215,8 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
 }
 // Bytes of workspace: for every share of every row its sums, maximum and sum of weights.  A window leaves fewer shares, never more.
 MOM_MX_FN size_t attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
-    const AttentionPlan p = attention_plan(T, B, Hq, Hkv, D, max_kv, 0);
-    const int64_t s = most_shares(max_kv, p.tiles);
+    const int64_t even = plan_shares(attention_plan(T, B, Hq, Hkv, D, max_kv, 0, false), max_kv), uneven = plan_shares(attention_plan(T, B, Hq, Hkv, D, max_kv, 0, true), max_kv);
+    const int64_t s = even > uneven ? even : uneven;
     return s <= 1 ? 0 : (size_t)s * (size_t)T * (size_t)Hq * (size_t)(D + 2) * 4;
 }
 

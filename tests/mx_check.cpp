@@ -1,7 +1,7 @@
 // Host-side check of what the four-bit kernels (csrc/mom_mx_*.hip.inc) take from csrc/mom_mx.h:
 //   1. a cache block's bytes: what the tokens append fills it, every nibble once, and what attention loads lies inside it;
 //   2. scales are the smallest that leave at most 7, and a number that is cut to 32 bits goes to the code of the whole one;
-//   3. tile numbers: every tile of every sequence has one of its own, all under the number of them;
+//   3. tile numbers: every tile of every sequence has one of its own, in their order, and the numbers behind them are none's;
 //   4. tokens: the steps of the wavefronts over all shares take every token that a tile sees once, pages are looked up inside the table,
 //      and the workspace holds the shares of every window.
 #include <cmath>
@@ -114,37 +114,39 @@ static void numbers(std::mt19937& rng) {
     std::vector<int> start(B + 1, 0);
     for (int b = 0; b < B; ++b) start[b + 1] = start[b] + (int)(rng() % 4 == 0 ? 0 : rng() % (rng() % 2 ? 4 : 300));
     const int64_t n = mx::tile_numbers(start[B], B, group, rows);
-    std::set<int64_t> used;
+    // the tile of a number as the kernel finds it: 64 sequences at a time, the first of them that has it
+    auto find = [&](const std::vector<int>& at, int64_t number) {
+        uint32_t before = 0;
+        for (int b = 0; b < B; ++b) {
+            const int s0 = std::min(std::max(at[b], 0), start[B]), m = std::min(std::max(at[b + 1], s0), start[B]) - s0;
+            const uint32_t tiles = mx::tiles_of(m, group, rows);
+            if ((uint32_t)number - before < tiles) return std::make_pair(mx::listed_tile((uint32_t)number, b, before, B, m, group, rows), m);
+            before += tiles;
+        }
+        return std::make_pair(mx::Tile{-1, 0}, 0);
+    };
+    int64_t next = 0;
     for (int b = 0; b < B; ++b) {
-        const int tiles = ((start[b + 1] - start[b]) * group + rows - 1) / rows;
-        for (int t = 0; t < tiles; ++t) {
-            const int64_t number = mx::first_tile(start[b], b, group, rows) + t;
-            CHECK(number >= 0 && number < n, "number %lld of %lld", (long long)number, (long long)n);
-            CHECK(used.insert(number).second, "number %lld twice", (long long)number);
-            // as the kernel finds it: the last sequence whose first number is not behind
-            int found = 0;
-            for (int i = 0; i < B; ++i) found += mx::first_tile(start[i], i, group, rows) <= number;
-            const mx::Tile of = mx::listed_tile(number, std::max(found, 1) - 1, start[std::max(found, 1) - 1], B, start[b + 1] - start[b], group, rows);
-            CHECK(of.b == b && of.tile == t, "number %lld is found in %d, not %d", (long long)number, of.b, b);
+        const int all = (start[b + 1] - start[b]) * group;
+        for (int t = 0; t * rows < all; ++t, ++next) {
+            CHECK(next < n, "number %lld of %lld", (long long)next, (long long)n);
+            const mx::Tile of = find(start, next).first;
+            CHECK(of.b == b && of.tile == t, "number %lld is tile %d of sequence %d, not %d of %d", (long long)next, of.tile, of.b, t, b);
         }
     }
-    // the numbers that are no tile's are none's; starts that are out of order name no sequence that is not there
+    // the numbers behind are none's; starts that are out of order name no sequence that is not there
     std::vector<int> wild(B + 1);
-    for (int& s : wild) s = (int)(rng() % (start[B] + 1));
+    for (int& s : wild) s = (int)(rng() % (start[B] + 3)) - 1;
     for (int64_t number = 0; number < n; ++number) {
-        for (int which = 0; which < 2; ++which) {
-            const std::vector<int>& at = which ? wild : start;
-            int found = 0;
-            for (int i = 0; i < B; ++i) found += mx::first_tile(at[i], i, group, rows) <= number;
-            const int b = std::max(found, 1) - 1, m = std::max(at[b + 1] - at[b], 0);
-            const mx::Tile of = mx::listed_tile(number, b, at[b], B, m, group, rows);
-            if (!which) CHECK((of.b >= 0) == (used.count(number) > 0), "number %lld", (long long)number);
-            if (of.b >= 0) CHECK(of.b < B && of.tile >= 0 && (int64_t)of.tile * rows < (int64_t)m * group, "number %lld: tile %d of sequence %d", (long long)number, of.tile, of.b);
-        }
+        if (number >= next) CHECK(find(start, number).first.b < 0, "number %lld", (long long)number);
+        const auto [of, m] = find(wild, number);
+        if (of.b >= 0) CHECK(of.b < B && of.tile >= 0 && (int64_t)of.tile * rows < (int64_t)m * group, "number %lld: tile %d of sequence %d", (long long)number, of.tile, of.b);
+        const mx::Tile any = mx::checked_tile(rng() % (2 * B), rng() % 64, B, m, group, rows);
+        if (any.b >= 0) CHECK(any.b < B && (int64_t)any.tile * rows < (int64_t)m * group, "tile %d of sequence %d", any.tile, any.b);
     }
     // sequences of m tokens each
     const int m = 1 + rng() % 300, each = (m * group + rows - 1) / rows;
-    const int64_t even = mx::tile_numbers((int64_t)B * m, B, group, rows);
+    const int64_t even = (int64_t)B * mx::tiles_of(m, group, rows) + 2;
     std::set<std::pair<int, int>> tiles;
     for (int64_t number = 0; number < even; ++number) {
         const mx::Tile of = mx::even_tile(number, B, m, group, rows);
@@ -160,12 +162,13 @@ static void tokens(std::mt19937& rng) {
     const int B = 1 + rng() % 8, m = 1 + rng() % (rng() % 2 ? 4 : 400);
     const int max_kv = rng() % (rng() % 2 ? 300 : 40000), window = rng() % 2 ? 0 : 1 + rng() % 3000;
     const int n = max_kv ? rng() % (max_kv + 1) : 0;
-    const mx::AttentionPlan p = mx::attention_plan((int64_t)B * m, B, Hkv * group, Hkv, D, max_kv, window);
+    const mx::AttentionPlan p = mx::attention_plan((int64_t)B * m, B, Hkv * group, Hkv, D, max_kv, window, rng() % 2);
     CHECK(p.share % mx::kStep == 0 && p.share > 0 && p.shares >= 1, "share %lld", (long long)p.share);
     if (p.shares > 1) {
         const size_t need = (size_t)p.shares * B * m * Hkv * group * (D + 2) * 4, have = mx::attention_workspace((int64_t)B * m, B, Hkv * group, Hkv, D, max_kv);
         CHECK(need <= have, "workspace %zu of %zu", need, have);
     }
+    CHECK(p.numbers >= (int64_t)B * mx::tiles_of(m, group, p.rows) && p.tiles >= (int64_t)B * Hkv, "numbers %lld, tiles %lld", (long long)p.numbers, (long long)p.tiles);
     const int all = m * group, table = (max_kv + page - 1) / page;
     const int tile = rng() % ((all + p.rows - 1) / p.rows);
     const int last_row = std::min((tile + 1) * p.rows, all) - 1;

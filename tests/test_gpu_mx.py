@@ -232,6 +232,13 @@ def test_many_short_sequences(Hq, Hkv, D):
     _compare(_gen(25), Hq, Hkv, D, 16, [1 + (7 * b) % 45 for b in range(B)], [1] * B)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (6, 1, 128), (4, 2, 256)])
+def test_many_sequences_of_their_own_numbers_of_tokens(Hq, Hkv, D):
+    """More than 64 sequences, some without tokens: tiles are counted over several rounds."""
+    asked = [(5 * b) % 12 if b % 7 else 0 for b in range(150)]
+    _compare(_gen(26), Hq, Hkv, D, 16, [a + (11 * b) % 60 for b, a in enumerate(asked)], asked)
+
+
 def test_rows_that_see_nothing():
     gen = _gen(15)
     # no tokens at all; fewer in the cache than asked about (the first stand before the beginning); lengths that are none

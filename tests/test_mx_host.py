@@ -36,9 +36,12 @@ def test_layout_encoding_tiles_and_shares(tmp_path):
     ("b -= 1;", "b -= 0;", "code"),
     ("- 127 - 2 + ((top", "- 127 - 3 + ((top", "scale"),
     ("> (3u << 21) ? 1 : 0", ">= (3u << 21) ? 1 : 0", "scale"),
-    ("{ return start * group / rows + b; }", "{ return start * group / rows; }", "number"),
-    ("if (b >= B || tile < 0", "if (tile < 0", "sequence"),
-    ("(uint32_t)tile >= (m * group + rows - 1) / rows)", "(uint32_t)tile > (m * group + rows - 1) / rows)", "number"),
+    ("{ return (m * group + rows - 1) / rows; }", "{ return (m * group + rows) / rows; }", "number"),
+    ("{ return T * group / rows + B; }", "{ return T * group / rows; }", "number"),
+    ("if (b >= B || tile >=", "if (tile >=", "sequence"),
+    ("tile >= tiles_of(m, group, rows))", "tile > tiles_of(m, group, rows))", "sequence"),
+    ("checked_tile(b, number - b * tiles,", "checked_tile(b, number,", "tile"),
+    ("checked_tile(b, number - before,", "checked_tile(b, number,", "number"),
     ("/ group) + 1;", "/ group);", "divided"),
     ("hi = p1 + 1;", "hi = p1;", "taken"),
     ("const int base = s.lo / kStep * kStep,", "const int base = s.lo / kStep * kStep + kStep,", "taken"),
