@@ -269,7 +269,8 @@ int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const 
  * Attention of T query tokens of B sequences over the cache: softmax(scale q k^T) v, q_heads / kv_heads query heads to a key head.
  *   q            [T][q_heads][head_dim] bf16 in, tokens q_stride elements apart (a multiple of 8), rotated already
  *   q_starts     [B + 1] device: the tokens of sequence b are q_starts[b] up to q_starts[b + 1], in order of their
- *                positions.  NULL: T / B tokens each (T a multiple of B).  Rows of `out` that belong to no sequence are not written.
+ *                positions.  NULL: T / B tokens each (T a multiple of B; the work is cut to their number then, so better
+ *                than starts that say the same).  Rows of `out` that belong to no sequence are not written.
  *   page_table   [B][table_stride] device: the pages of each sequence.  The tokens of a page that is none of the cache's
  *                count as not seen.
  *   kv_lens      [B] device: tokens of each sequence in the cache, the new ones among them; at most max_kv and
@@ -282,7 +283,9 @@ int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const 
  *   workspace    at least mom_mx_attention_workspace_bytes(T, B, q_heads, kv_heads, head_dim, max_kv) bytes, 16-byte
  *                aligned (NULL where that is 0)
  * Arithmetic: products of bf16 numbers with fp32 sums on the matrix cores, softmax in fp32, its weights rounded to bf16 for
- * the second product, one rounding of the result.  What a row does not see does not reach it, NaN included.
+ * the second product (where tiles of rows are few, what that takes off is multiplied too), one rounding of the result.
+ * What a row does not see does not reach it, NaN included.
+ * Extents: T, B and max_kv up to 2^29, heads under 2^15, T * q_heads up to 2^31 - 65536.
  */
 size_t mom_mx_attention_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_kv);
 int mom_mx_attention(const void *q, int64_t q_stride, const int32_t *q_starts, int64_t T, int64_t B,
