@@ -135,6 +135,8 @@ def main():
     p.add_argument("--heads", type=int, default=32)
     p.add_argument("--kv-heads", type=int, default=8)
     a = p.parse_args()
+    if a.prompt < 1 or a.tokens < 1:
+        p.error("--prompt and --tokens are at least 1")
     layer = Layer(a.hidden, a.intermediate, a.heads, a.kv_heads, 128, a.prompt + a.tokens)
     x = torch.randn((a.prompt, a.hidden), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
     host, side = torch.empty(layer.cache.numel(), dtype=torch.uint8, pin_memory=True), torch.cuda.Stream()
@@ -157,7 +159,7 @@ def main():
         graph.replay()
         t = step_out.clone()
     torch.cuda.synchronize()
-    each = (time.perf_counter() - begun) / max(a.tokens, 1)
+    each = (time.perf_counter() - begun) / a.tokens
     print(f"{a.prompt} tokens of prompt, {a.tokens} decoded: {each * 1e6:.1f} us a token of one layer; last token rms {t.float().pow(2).mean().sqrt().item():.3f}")
 
 
