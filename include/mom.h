@@ -268,9 +268,10 @@ int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const 
 /*
  * Attention of T query tokens of B sequences over the cache: softmax(scale q k^T) v, q_heads / kv_heads query heads to a key head.
  *   q            [T][q_heads][head_dim] bf16 in, tokens q_stride elements apart (a multiple of 8), rotated already
- *   q_starts     [B + 1] device: the tokens of sequence b are q_starts[b] up to q_starts[b + 1], in order of their
+ *   q_starts     [B + 1] device, ascending: the tokens of sequence b are q_starts[b] up to q_starts[b + 1], in order of their
  *                positions.  NULL: T / B tokens each (T a multiple of B; the work is cut to their number then, so better
- *                than starts that say the same).  Rows of `out` that belong to no sequence are not written.
+ *                than starts that say the same).  Rows of `out` and `lse` that belong to no sequence, in front of q_starts[0] and from
+ *                q_starts[B] on, are not written.  (Starts that do not ascend leave rows without a meaning; nothing out of range is touched.)
  *   page_table   [B][table_stride] device: the pages of each sequence.  The tokens of a page that is none of the cache's
  *                count as not seen.
  *   kv_lens      [B] device: tokens of each sequence in the cache, the new ones among them; at most max_kv and

@@ -1,0 +1,89 @@
+"""Attention over the four-bit cache where a call's shares, page numbers and forms meet: against 64 bits (tests/mx_attention_bounds.py), on keys and
+values that mom_mx_kv_append stores and mom_mx_kv_read reads back."""
+import math
+
+import pytest
+import torch
+
+import mx_attention_bounds as bounds
+import mx_reference as ref
+from paper_2504_12526_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _fill(gen, Hkv, D, P, lens, max_kv, values=1.0):
+    """A cache whose pages are in any order, noise (NaN among it) wherever nothing is stored; the table, and each sequence's keys and values."""
+    each = -(-max_kv // P)
+    pool = torch.randperm(sum(-(-n // P) for n in lens) + 3, generator=gen)
+    table, used = torch.full((len(lens), each), -1, dtype=torch.int32), 0
+    for b, n in enumerate(lens):
+        table[b, :-(-n // P)] = pool[used:used + -(-n // P)]
+        used += -(-n // P)
+    cache = torch.randint(0, 256, (len(pool), Hkv, ref.block_bytes(P, D)), generator=gen, dtype=torch.uint8).to(DEV)
+    slots = torch.cat([table[b].long()[torch.arange(n) // P] * P + torch.arange(n) % P for b, n in enumerate(lens)]).to(DEV)
+    k, v = (torch.randn((len(slots), Hkv, D), generator=gen).to(torch.bfloat16).to(DEV) for _ in range(2))
+    binding.mom_mx_kv_append(k, v * values, slots, cache, P)
+    binding.mom_mx_kv_read(cache, P, slots, k, v)
+    return cache, table, [t.double() for t in k.cpu().split(lens)], [t.double() for t in v.cpu().split(lens)]
+
+
+def _run(q, cache, P, table, lens, max_kv, starts=None, scale=None, window=0):
+    (T, Hq, D), Hkv = q.shape, cache.shape[1]
+    out, lse = torch.full((T, Hq, D), 3.0, dtype=torch.bfloat16, device=DEV), torch.full((T, Hq), 3.0, device=DEV)
+    n = binding.mom_mx_attention_workspace_bytes(T, table.shape[0], Hq, Hkv, D, max_kv)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device=DEV) if n else None            # NaN wherever nothing is written
+    starts = None if starts is None else torch.tensor(starts, dtype=torch.int32, device=DEV)
+    binding.mom_mx_attention(q.to(DEV), cache, P, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), max_kv, out, ws, q_starts=starts, scale=scale,
+                             window=window, lse=lse)
+    return out, lse, n
+
+
+def _near(lse, z, err):
+    lse, seen = lse.double().cpu(), torch.isfinite(z)
+    assert torch.equal(lse[~seen], z[~seen]) and float(((lse - z).abs() - err)[seen].max()) <= 0
+
+
+def _compare(seed, Hq, Hkv, D, P, lens, asked, max_kv=None, window=0, shared=None, listed=True, std=1.0, weights=bounds.ROUNDED):
+    gen = torch.Generator().manual_seed(seed)
+    max_kv = max(lens) if max_kv is None else max_kv
+    cache, table, keys, values = _fill(gen, Hkv, D, P, lens, max_kv)
+    starts = [0] + torch.tensor(asked).cumsum(0).tolist()
+    q = (torch.randn((starts[-1], Hq, D), generator=gen) * std).to(torch.bfloat16)
+    out, lse, workspace = _run(q, cache, P, table, lens, max_kv, starts if listed else None, None, window)
+    if shared is not None:
+        assert (workspace > 0) == shared
+    want, z, err, z_err = bounds.attention(q, keys, values, starts, lens, 1 / math.sqrt(D), window, weights)
+    assert bounds.outside(out, want, err) == 0
+    _near(lse, z, z_err)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 1, 64), (4, 2, 256)])
+@pytest.mark.parametrize("starts,T", [([0, 2, 5], 9), ([3, 4, 6], 8), ([1, 1, 3], 3)])
+def test_tokens_of_no_sequence_are_left_alone_where_shares_are_joined(Hq, Hkv, D, starts, T):
+    gen = torch.Generator().manual_seed(1)
+    lens = [3000, 40]
+    cache, table, keys, values = _fill(gen, Hkv, D, 16, lens, 3000)
+    q = torch.randn((T, Hq, D), generator=gen).to(torch.bfloat16)
+    out, lse, workspace = _run(q, cache, 16, table, lens, 3000, starts)
+    assert workspace > 0
+    want, z, err, z_err = bounds.attention(q, keys, values, starts, lens, 1 / math.sqrt(D))
+    inside = slice(starts[0], starts[-1])
+    assert bounds.outside(out[inside], want[inside], err[inside]) == 0
+    _near(lse[inside], z[inside], z_err[inside])
+    none = [i for i in range(T) if not starts[0] <= i < starts[-1]]
+    assert (out[none] == 3).all() and (lse[none] == 3).all()
+
+
+def test_rows_of_no_sequence_beside_a_chunk_in_shares():
+    gen = torch.Generator().manual_seed(2)
+    starts, T, lens, D = [20, 120], 150, [3000], 128
+    cache, table, keys, values = _fill(gen, 1, D, 64, lens, 3000)
+    q = torch.randn((T, 4, D), generator=gen).to(torch.bfloat16)
+    out, lse, workspace = _run(q, cache, 64, table, lens, 3000, starts)
+    assert workspace > 0
+    want, _, err, _ = bounds.attention(q, keys, values, starts, lens, 1 / math.sqrt(D))
+    assert bounds.outside(out[20:120], want[20:120], err[20:120]) == 0
+    none = list(range(20)) + list(range(120, T))
+    assert (out[none] == 3).all() and (lse[none] == 3).all()
