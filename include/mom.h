@@ -297,7 +297,7 @@ int mom_mx_attention(const void *q, int64_t q_stride, const int32_t *q_starts, i
                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* Encodes a weight w [N,K] bf16 (K a positive multiple of 32, at most 32768): codes [N][K / 2] (16-byte aligned), low nibble
- * first, and scales [N][K / 32]. */
+ * first, and scales [N][K / 32] (at any byte, here and in the products: rows cut out of a weight are one too). */
 int mom_mx_quantize(const void *w, int64_t N, int64_t K, void *codes, void *scales, void *stream);
 
 /*

@@ -87,3 +87,24 @@ def test_rows_of_no_sequence_beside_a_chunk_in_shares():
     assert bounds.outside(out[20:120], want[20:120], err[20:120]) == 0
     none = list(range(20)) + list(range(120, T))
     assert (out[none] == 3).all() and (lse[none] == 3).all()
+
+
+@pytest.mark.parametrize("M", [1, 5, 16])
+@pytest.mark.parametrize("N,K", [(300, 1056), (70, 64), (40, 4096), (33, 14336), (32900, 96)])
+@pytest.mark.parametrize("offset", [1, 6, 13])
+def test_scales_at_any_byte(M, N, K, offset):
+    """Rows cut out of a larger weight: codes on 16 bytes, scales anywhere."""
+    gen = torch.Generator().manual_seed(11)
+    x = torch.randn((M, K), generator=gen).to(torch.bfloat16).to(DEV)
+    codes = torch.randint(0, 256, (N, K // 2), generator=gen, dtype=torch.uint8).to(DEV)
+    scales = torch.randint(118, 126, (N, K // 32), generator=gen, dtype=torch.uint8).to(DEV)
+    moved = torch.full((scales.numel() + 32,), 255, dtype=torch.uint8, device=DEV)[offset:offset + scales.numel()].view_as(scales)
+    moved.copy_(scales)
+    want, got = (torch.empty((M, N), device=DEV) for _ in range(2))
+    binding.mom_mx_matvec(x, codes, scales, want)
+    binding.mom_mx_matvec(x, codes, moved, got)
+    assert torch.isfinite(want).all() and torch.equal(got, want)
+    want, got = (torch.empty((M, N), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    binding.mom_mx_gateup(x, codes, scales, codes, scales, want)
+    binding.mom_mx_gateup(x, codes, moved, codes, moved, got)
+    assert torch.equal(got.view(torch.int16), want.view(torch.int16))
