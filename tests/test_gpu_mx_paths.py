@@ -89,6 +89,21 @@ def test_rows_of_no_sequence_beside_a_chunk_in_shares():
     assert (out[none] == 3).all() and (lse[none] == 3).all()
 
 
+def test_a_table_beside_the_result():
+    """Rows of a page table that lie apart: what lies between and behind them is not the table's, and may be the result's."""
+    gen = torch.Generator().manual_seed(10)
+    D, P, lens, starts = 64, 16, [64, 37], [0, 1, 2]
+    cache, table, keys, values = _fill(gen, 1, D, P, lens, 64)
+    buf = torch.full((4096,), -1, dtype=torch.int32, device=DEV)
+    wide = buf[:128 + 4].as_strided((2, 4), (128, 1))         # four pages a row, 128 entries from row to row
+    wide.copy_(table)
+    out = buf[136:136 + 2 * 2 * D // 2].view(torch.bfloat16).view(2, 2, D)
+    q = torch.randn((2, 2, D), generator=gen).to(torch.bfloat16)
+    binding.mom_mx_attention(q.to(DEV), cache, P, wide, torch.tensor(lens, dtype=torch.int32, device=DEV), 64, out, None)
+    want, _, err, _ = bounds.attention(q, keys, values, starts, lens, 1 / math.sqrt(D))
+    assert bounds.outside(out, want, err) == 0
+
+
 @pytest.mark.parametrize("M", [1, 5, 16])
 @pytest.mark.parametrize("N,K", [(300, 1056), (70, 64), (40, 4096), (33, 14336), (32900, 96)])
 @pytest.mark.parametrize("offset", [1, 6, 13])
