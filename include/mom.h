@@ -273,7 +273,7 @@ int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const 
  *                than starts that say the same).  Rows of `out` and `lse` that belong to no sequence, in front of q_starts[0] and from
  *                q_starts[B] on, are not written.  (Starts that do not ascend leave rows without a meaning; nothing out of range is touched.)
  *   page_table   [B][table_stride] device: the pages of each sequence; the last row may end with the pages that max_kv takes.  The
- *                tokens of a page that is none of the cache's count as not seen.
+ *                tokens of a page that is none of the cache's count as not seen.  May be NULL where there are none (max_kv or table_stride 0).
  *   kv_lens      [B] device: tokens of each sequence in the cache, the new ones among them; at most max_kv and
  *                table_stride * page_tokens of them count
  *   max_kv       host: no length is above it.  The work is shared out by it, so the nearer the better.

@@ -104,6 +104,14 @@ def test_a_table_beside_the_result():
     assert bounds.outside(out, want, err) == 0
 
 
+def test_a_table_without_pages():
+    """No pages yet: nothing is seen."""
+    cache = torch.zeros((1, 1, ref.block_bytes(16, 64)), dtype=torch.uint8, device=DEV)
+    q, out, lse = torch.ones((2, 2, 64), dtype=torch.bfloat16, device=DEV), torch.full((2, 2, 64), 3.0, dtype=torch.bfloat16, device=DEV), torch.full((2, 2), 3.0, device=DEV)
+    binding.mom_mx_attention(q, cache, 16, torch.empty((2, 0), dtype=torch.int32, device=DEV), torch.tensor([5, 0], dtype=torch.int32, device=DEV), 64, out, None, lse=lse)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+
+
 @pytest.mark.parametrize("M", [1, 5, 16])
 @pytest.mark.parametrize("N,K", [(300, 1056), (70, 64), (40, 4096), (33, 14336), (32900, 96)])
 @pytest.mark.parametrize("offset", [1, 6, 13])
