@@ -253,7 +253,8 @@ size_t mom_mx_block_bytes(int64_t head_dim, int64_t page_tokens);      /* 0 for 
  *              head_dim; 0: nothing is rotated, and both may be NULL
  *   interleaved  0: the pairs are dimensions (i, i + rot_dim / 2); else (2 i, 2 i + 1)
  *   q_out      [T][q_heads][head_dim] bf16 out, dense; may be q itself where that is dense too
- * The rotation runs in 64 bits: queries are rounded once, keys go from there to four bits.
+ * The rotation runs in 64 bits: queries are rounded once, keys go from there to four bits.  T is at most 2^26 - 4, here and for
+ * mom_mx_kv_read.
  */
 int mom_mx_kv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                      const int64_t *slots, const int32_t *positions, const float *inv_freq, int64_t rot_dim, int interleaved,
@@ -286,7 +287,8 @@ int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const 
  * Arithmetic: products of bf16 numbers with fp32 sums on the matrix cores, softmax in fp32, its weights rounded to bf16 for
  * the second product (where tiles of rows are few, what that takes off is multiplied too), one rounding of the result.
  * What a row does not see does not reach it, NaN included.
- * Extents: T, B and max_kv up to 2^29, heads under 2^15, T * q_heads up to 2^31 - 65536.
+ * Extents: T, B and max_kv up to 2^29, heads under 2^15, T * q_heads up to 2^31 - 65536, and the tiles of rows that a launch holds: a call with
+ * T * q_heads / 16 + B * kv_heads under 2^23 has no more.
  */
 size_t mom_mx_attention_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_kv);
 int mom_mx_attention(const void *q, int64_t q_stride, const int32_t *q_starts, int64_t T, int64_t B,
@@ -297,13 +299,14 @@ int mom_mx_attention(const void *q, int64_t q_stride, const int32_t *q_starts, i
                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* Encodes a weight w [N,K] bf16 (K a positive multiple of 32, at most 32768): codes [N][K / 2] (16-byte aligned), low nibble
- * first, and scales [N][K / 32] (at any byte, here and in the products: rows cut out of a weight are one too). */
+ * first, and scales [N][K / 32] (at any byte, here and in the products: rows cut out of a weight are one too).
+ * N * K is at most 2^35 - 2^11. */
 int mom_mx_quantize(const void *w, int64_t N, int64_t K, void *codes, void *scales, void *stream);
 
 /*
  * y = x W^T (+ residual) for one to MOM_MX_MAX_ROWS tokens and a weight in four bits, as mom_mx_quantize lays it out.
  *   x [M,K] bf16 in;  out [M,N] fp32 (out_fp32 not 0) or bf16;  residual [M,N] bf16 or NULL, with bf16 only (may be `out` itself)
- * fp32 sums, one rounding.  A weight in bf16 takes 3.76 times the bytes: mom_lmhead_last, mom_mlp_last.
+ * fp32 sums, one rounding.  N is at most 2^26 - 16 (mom_mx_gateup too; more is refused where a launch does not hold it).  A weight in bf16 takes 3.76 times the bytes: mom_lmhead_last, mom_mlp_last.
  */
 #define MOM_MX_MAX_ROWS 16
 int mom_mx_matvec(const void *x, int64_t M, const void *codes, const void *scales, int64_t N, int64_t K,
