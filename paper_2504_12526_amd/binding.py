@@ -112,11 +112,17 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# torch's own questions for the current device and its current stream's handle, which have no public names; None where torch has no such function.
+_current_device, _current_handle = (getattr(torch._C, name, None) for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
+
+
 def _stream(stream):
-    """Handle of a stream, None: the current one of the current device (asked by its number: a torch Stream object takes 4 us to make, which is
-    more than a small kernel)."""
+    """Handle of a stream, None: the current one of the current device (asked by its number where torch answers that: a torch Stream object
+    takes 4 us to make, which is more than a small kernel)."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if _current_device is not None and _current_handle is not None:
+            return _current_handle(_current_device())
+        stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
 
