@@ -89,6 +89,71 @@ def test_rows_of_no_sequence_beside_a_chunk_in_shares():
     assert (out[none] == 3).all() and (lse[none] == 3).all()
 
 
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 64), (256, 32)])
+@pytest.mark.parametrize("lens,asked,max_kv,window", [([3000], [100], 3000, 0), ([3000], [100], 3000, 700), ([700], [100], 3000, 0), ([2900, 60, 1500], [90, 70, 101], 2900, 0),
+                                                      ([2000], [90], 2000, 1)])
+def test_many_rows_in_shares(D, P, lens, asked, max_kv, window):
+    """Parts of the tokens, empty ones among them, for wavefronts with and without rows; past 1024 tokens the page numbers are looked up again."""
+    _compare(3, 4, 1, D, P, lens, asked, max_kv, window, shared=True)
+
+
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 128), (256, 16)])
+def test_many_rows_in_one_share_past_1024_tokens(D, P):
+    _compare(4, 130, 130, D, P, [1300], [258], shared=False)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,m,listed,shared", [(8, 8, 64, 1, True, False), (8, 8, 128, 1, False, False), (8, 8, 256, 1, True, False),
+                                                      # (of 20 rows each; the workspace is the larger one of sequences with and without starts)
+                                                      (12, 3, 64, 5, True, None), (12, 3, 128, 5, True, None), (16, 4, 128, 5, False, None)])
+def test_more_than_32_steps_of_a_wavefront(Hq, Hkv, D, m, listed, shared):
+    """Many tiles and one sequence of more than 8192 tokens, in one share: the page numbers are looked up again."""
+    B = 64
+    _compare(5, Hq, Hkv, D, 16, [9300] + [m + (7 * b) % 50 for b in range(1, B)], [m] * B, listed=listed, shared=shared)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_more_than_32_steps_of_a_wavefront_in_shares(D):
+    B = 63
+    _compare(7, 2, 1, D, 256, [72000] + [1 + 5 * b for b in range(1, B)], [1] * B, shared=True)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 128), (4, 1, 64), (7, 1, 128)])
+@pytest.mark.parametrize("lens,asked,max_kv,window", [([2500, 300], [7, 9], 2500, 0), ([2500, 300], [7, 9], 2500, 1300), ([400], [12], 2500, 0)])
+def test_a_few_rows_in_shares(Hq, Hkv, D, lens, asked, max_kv, window):
+    _compare(8, Hq, Hkv, D, 16, lens, asked, max_kv, window, shared=True)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens,asked", [(8, 1, 64, [64], [1]), (16, 1, 128, [64], [1]), (4, 2, 128, [70, 33, 64], [1, 1, 1]), (8, 1, 256, [60], [1]), (20, 1, 256, [50], [1]),
+                                                 (4, 1, 64, [64], [3]), (4, 4, 256, [64] * 15, [1] * 15), (40, 10, 128, [61] * 6, [1] * 6)])
+def test_few_tiles_of_few_rows_have_the_rounding_of_the_result_alone(Hq, Hkv, D, lens, asked):
+    """Up to 16 rows a sequence (any number up to 256 where there are 256 dimensions) and fewer than 64 tiles: weights near one another, so that what they lose
+    by their rounding to bf16 shows in the result."""
+    _compare(9, Hq, Hkv, D, 16, lens, asked, std=0.1, weights=bounds.WITH_REST)
+
+
+@pytest.mark.parametrize("kind", ["keys", "values"])
+def test_append_of_numbers_below_the_smallest_scale(kind):
+    """Subnormal bf16 numbers, which 2^-125 brings to at most half a step of the largest, and zeros."""
+    D, P = 64, 16
+    bits = torch.arange(0, 256, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = torch.zeros(4, 1, D, dtype=torch.bfloat16)
+    x[0, 0, :], x[1, 0, :], x[2, 0, :], x[3, 0, :] = bits[:64], bits[64:128], -bits[128:192], bits[192:256]
+    y = torch.ones_like(x)
+    k, v = (x, y) if kind == "keys" else (y, x)
+    cache = torch.zeros(1, 1, ref.block_bytes(P, D), dtype=torch.uint8)
+    got = cache.to(DEV)
+    binding.mom_mx_kv_append(k.to(DEV), v.to(DEV), torch.arange(4).to(DEV), got, P)
+    assert torch.equal(got.cpu(), ref.append(cache, P, k.double(), v.double(), torch.arange(4)))
+
+
+def test_quantize_of_numbers_below_the_smallest_scale():
+    w = torch.arange(0, 256, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(4, 64).clone()
+    codes, scales = torch.empty((4, 32), dtype=torch.uint8, device=DEV), torch.empty((4, 2), dtype=torch.uint8, device=DEV)
+    binding.mom_mx_quantize(w.to(DEV), codes, scales)
+    c, s = ref.encode(w.double())
+    assert torch.equal(codes.cpu(), ref.pack(c)) and torch.equal(scales.cpu(), s.to(torch.uint8))
+
+
 def test_a_table_beside_the_result():
     """Rows of a page table that lie apart: what lies between and behind them is not the table's, and may be the result's."""
     gen = torch.Generator().manual_seed(10)
