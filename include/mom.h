@@ -226,7 +226,7 @@ int mom_kv_reload(const void *pinned_host, void *k, void *v, void *stream, size_
  *
  * What the library encodes gets the power of two that brings the largest magnitude of its block to at most 7 (between
  * 2^-125 and 2^125), and each element the nearest code, ties to the even one: at most half a step off, nothing
- * cut off.  A block with an infinity or a NaN becomes NaN as a whole.  Values that are read back are exact in bf16.
+ * cut off up to 7 * 2^125 (bf16 ends just under 8 * 2^125).  A block with an infinity or a NaN becomes NaN as a whole.  Values that are read back are exact in bf16.
  *
  * The cache of a layer is one device buffer [pages][kv_heads] of blocks of mom_mx_block_bytes(head_dim, page_tokens)
  * bytes, 16-byte aligned: page_tokens (16, 32, 64, 128 or 256) tokens of one key head, head_dim 64, 128 or 256.  A
@@ -253,7 +253,7 @@ size_t mom_mx_block_bytes(int64_t head_dim, int64_t page_tokens);      /* 0 for 
  *              head_dim; 0: nothing is rotated, and both may be NULL
  *   interleaved  0: the pairs are dimensions (i, i + rot_dim / 2); else (2 i, 2 i + 1)
  *   q_out      [T][q_heads][head_dim] bf16 out, dense; may be q itself where that is dense too
- * The rotation runs in 64 bits: queries are rounded once, keys go from there to four bits.  T is at most 2^26 - 4, here and for
+ * The rotation runs in 64 bits: queries are rounded to bf16 by way of 32 bits, keys go from there to four bits.  T is at most 2^26 - 4, here and for
  * mom_mx_kv_read.
  */
 int mom_mx_kv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
@@ -283,9 +283,13 @@ int mom_mx_kv_read(const void *cache, int64_t pages, int64_t page_tokens, const 
  *   out          [T][q_heads][head_dim] bf16, dense;  lse [T][q_heads] fp32 or NULL: log sum exp of the scaled scores.
  *                A row that sees nothing is 0, its lse -infinity.
  *   workspace    at least mom_mx_attention_workspace_bytes(T, B, q_heads, kv_heads, head_dim, max_kv) bytes, 16-byte
- *                aligned (NULL where that is 0)
+ *                aligned (NULL where that is 0).  More max_kv never takes less, but fewer tokens may take more, being cut into more
+ *                shares: one buffer for calls of several T and B is the largest of their sizes
  * Arithmetic: products of bf16 numbers with fp32 sums on the matrix cores, softmax in fp32, its weights rounded to bf16 for
- * the second product (where tiles of rows are few, what that takes off is multiplied too), one rounding of the result.
+ * the second product, one rounding of the result (2.3e-3 of the norm off; the result's rounding alone is 1.7e-3).  What the weights lose is
+ * multiplied too, and only the result's rounding is left, where the rows of a sequence at one key head (its tokens times q_heads / kv_heads) are
+ * up to 16 on average, with head_dim 256 up to 256, and there are fewer than 64 tiles of 16 of them in all.  How tokens are shared out goes by the
+ * extents too: the same sequence has the same bits in calls of the same extents, not beside other numbers of sequences.
  * What a row does not see does not reach it, NaN included.
  * Extents: T, B and max_kv up to 2^29, heads under 2^15, T * q_heads up to 2^31 - 65536, and the tiles of rows that a launch holds: a call with
  * T * q_heads / 16 + B * kv_heads under 2^23 has no more.

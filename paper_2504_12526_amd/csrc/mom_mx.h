@@ -38,7 +38,8 @@ MOM_MX_FN bool finite(uint32_t magnitude) { return magnitude < 0x7f800000u; }
 
 // Exponent of the scale of a block whose largest magnitude is `top` (finite): the power of two that brings it to at most 7, which is half a step
 // away from the largest element 6, so that no element is further than half a step from its code (the rounding down to [4, 8) that is
-// also in use cuts off up to a quarter of the largest element).
+// also in use cuts off up to a quarter of the largest element).  Above 7 * 2^125
+// (the largest number of bf16 is just under 8 * 2^125) 6 * 2^125 stands for everything.
 MOM_MX_FN int scale_exponent(uint32_t top) {
     const int e = (int)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > (3u << 21) ? 1 : 0);
     return e < kMinExponent ? kMinExponent : e > kMaxExponent ? kMaxExponent : e;
@@ -213,7 +214,8 @@ MOM_MX_FN AttentionPlan attention_plan(int64_t T, int64_t B, int Hq, int Hkv, in
     p.shares = reach > 0 ? (int)((reach + p.share - 1) / p.share) : 1;
     return p;
 }
-// Bytes of workspace: for every share of every row its sums, maximum and sum of weights.  A window leaves fewer shares, never more.
+// Bytes of workspace: for every share of every row its sums, maximum and sum of weights.  A window or a shorter reach leaves fewer shares, never more; fewer
+// tokens may be cut into more of them.
 MOM_MX_FN size_t attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
     const int64_t even = plan_shares(attention_plan(T, B, Hq, Hkv, D, max_kv, 0, false), max_kv), uneven = plan_shares(attention_plan(T, B, Hq, Hkv, D, max_kv, 0, true), max_kv);
     const int64_t s = even > uneven ? even : uneven;

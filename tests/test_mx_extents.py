@@ -38,3 +38,12 @@ def test_gate_and_up_of_too_many_rows(M, N, K):
 @pytest.mark.parametrize("N,K", [(1 << 20, 32768), (0x7fffff00, 32), (0x7fffff00, 4096)])
 def test_quantize_of_too_many_blocks(N, K):
     assert binding.lib().mom_mx_quantize(A[0], N, K, A[1], A[2], None) == SHAPE
+
+
+def test_workspace_never_shrinks_with_max_kv():
+    """So what a query says for max_kv is enough wherever a table holds fewer tokens."""
+    wb = binding.lib().mom_mx_attention_workspace_bytes
+    for T, B, q_heads, kv_heads, D in ((1, 1, 32, 8, 128), (32, 32, 32, 8, 128), (35, 7, 28, 4, 128), (64, 4, 16, 1, 64), (300, 3, 8, 2, 256), (2048, 1, 32, 8, 128), (2055, 8, 32, 8, 128),
+                                       (700, 100, 16, 16, 64), (1, 1, 1, 1, 64), (5000, 2, 4, 4, 256)):
+        sizes = [wb(T, B, q_heads, kv_heads, D, n) for n in [*range(0, 9000, 37), *range(9000, 1 << 20, 7001)]]
+        assert sizes == sorted(sizes), (T, B, q_heads, kv_heads, D)
