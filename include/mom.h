@@ -322,6 +322,82 @@ int mom_mx_gateup(const void *x, int64_t M, const void *gate_codes, const void *
                   const void *up_codes, const void *up_scales, int64_t N, int64_t K, void *out, void *stream);
 
 /*
+ * Drafted tokens in a tree.  Some new tokens of a sequence, its rows, form a tree: row 0 is the last token that is certain, the others are drafts, and a row's parent is the row that it
+ * continues.  All rows are appended (mom_mx_kv_append) and attended (mom_mx_tree_attention) at once, row i as token n - m + i of the n in the cache, m rows among them; the
+ * target's logits of all of them say which stay (mom_verify_drafts), and those are moved together (mom_mx_kv_keep).
+ *   q_starts     [B + 1] device, ascending: sequence b has the rows q_starts[b] up to q_starts[b + 1]; NULL: T / B rows each (T a multiple of B).  Rows
+ *                in front of q_starts[0] and from q_starts[B] on belong to no sequence: nothing is written there
+ *   parents      [T] device: the number of each row's parent within its sequence, a lower one than its own; -1, and what is no lower number: none.
+ *                NULL: chains, each row the child of the one before it
+ *   MOM_MAX_DRAFT_ROWS  rows of a sequence that masks and verification know: those behind are seen by none and never taken
+ */
+#define MOM_MAX_DRAFT_ROWS 512
+
+/*
+ * The tree as the other calls take it, once for all layers of a step.  Any of the three outputs may be NULL.
+ *   kv_lens      [B] device: tokens of each sequence in the cache, the rows among them
+ *   page_table, table_stride, page_tokens, max_kv   as in mom_mx_attention, for slots
+ *   masks        [T][mask_words] 32-bit words out (mask_words 1 to MOM_MAX_DRAFT_ROWS / 32): bit j % 32 of word j / 32 says that the row sees row j, itself
+ *                and those above it
+ *   positions    [T] out: n - m + the number of rows above this one, for the rotation in mom_mx_kv_append
+ *   slots        [T] out: where the row goes in the cache; -1 where its place is before the sequence or past max_kv, or the page is negative
+ */
+int mom_mx_tree(const int32_t *parents, const int32_t *q_starts, int64_t T, int64_t B, const int32_t *kv_lens,
+                const int32_t *page_table, int64_t table_stride, int64_t page_tokens, int64_t max_kv,
+                void *masks, int64_t mask_words, int32_t *positions, int64_t *slots, void *stream);
+
+/*
+ * mom_mx_attention for rows of trees: a row sees the tokens in front of its sequence's rows, and of the rows those whose bit is set in its mask (masks need not be
+ * trees'; a row whose mask is empty sees what is in front, and is 0 with lse -infinity where that is nothing).
+ *   masks, mask_words   as mom_mx_tree writes them; rows past the last word are not seen
+ *   window       0, or how many tokens a row sees at most: the last ones, in the order of the cache, of those that it would see
+ * Everything else as in mom_mx_attention, the workspace by this call's own query.
+ */
+size_t mom_mx_tree_attention_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_kv);
+int mom_mx_tree_attention(const void *q, int64_t q_stride, const int32_t *q_starts, int64_t T, int64_t B,
+                          int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                          const void *cache, int64_t pages, int64_t page_tokens,
+                          const int32_t *page_table, int64_t table_stride, const int32_t *kv_lens,
+                          int64_t max_kv, float scale, int64_t window, const void *masks, int64_t mask_words,
+                          void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Which drafted tokens stay, and the next token.  At a row, from row 0 on, p = softmax(target / t) and q = softmax(draft / t), r = p, and its children x in the order of their rows:
+ *     u q(x) < r(x)   the child is taken, and the same begins there;   otherwise   r <- max(r - q, 0) / sum max(r - q, 0)
+ * with the child's number u.  Where no child is taken the next token is drawn from r: the first whose cumulative sum is above u times the whole sum, u the number of
+ * row 0.  If the children were drawn from q, independently, what comes out is distributed as tokens drawn from the target one by one.  One row a sequence: drawing from the target.
+ *   target       [T][V] fp32 (logits_bf16 not 0: bf16) logits, rows target_stride elements apart
+ *   draft        [T][V] the drafting model's logits at the same rows, same type, draft_stride apart, read where a row has children; NULL: drafts without
+ *                probabilities, q(x) = 1 (r loses the refused token alone)
+ *   tokens       [T] each row's token; that of row 0 is not looked at
+ *   max_children children of a row that are tried, at least 1; more than there are cost two launches each where `draft` is given
+ *   temperatures [B] device, t of each sequence, NULL: 1; not above 0: greedy, a child is taken if it is the target's largest logit, which is the next token too
+ *   uniforms     [T] numbers in [0, 1): those of rows 1 ... for their drafts, that of row 0 for the next token
+ *   rows         [T] out: per sequence from its first row on, the rows that stay: row 0, and down the tree
+ *   out_tokens   [T] out: the tokens taken, and behind them the next token
+ *   counts       [B] out: rows that stay, at least 1, and so many tokens; 0 for a sequence without rows.  What is left of rows and out_tokens is -1
+ * A row whose token is none of the vocabulary, or that has no parent, is not tried.  Of equal largest logits the lowest counts.  A NaN counts as -infinity, +infinity as the largest number; where
+ * all logits are -infinity nothing is taken and the next token is -1.  Where refusals leave nothing (numbers of 1 or more) it is drawn from p.
+ * Everything is in 64 bits from the logits on.  T rows, B and V under 2^29, 2^29 and 2^30, and what a launch holds.  Workspace 16-byte aligned.
+ */
+size_t mom_verify_drafts_workspace_bytes(int64_t T, int64_t B, int64_t V);
+int mom_verify_drafts(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride, int logits_bf16, int64_t V,
+                      const int32_t *tokens, const int32_t *parents, int64_t max_children, const int32_t *q_starts, int64_t T, int64_t B,
+                      const float *temperatures, const float *uniforms, int32_t *rows, int32_t *out_tokens, int32_t *counts,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The rows that stay moved together in a layer's cache: token n - m + rows[i] of sequence b goes to the place n - m + i, for i under counts[b] (at most m).
+ * rows and counts as mom_verify_drafts writes them: rising, and no row lower than its place (a row that is neither, or none of the sequence's, is not moved; nothing out of range is
+ * touched).  Tokens whose place or page is none of the cache's stay, too.
+ *   page_table, table_stride, page_tokens, max_kv, kv_lens   as before the call: the rows among the tokens
+ *   new_lens     [B] out: n - m + counts[b], what the cache holds of the sequence now; another buffer than kv_lens, which the other layers' calls still need
+ */
+int mom_mx_kv_keep(void *cache, int64_t pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim,
+                   const int32_t *page_table, int64_t table_stride, int64_t max_kv, const int32_t *kv_lens, const int32_t *q_starts,
+                   int64_t T, int64_t B, const int32_t *rows, const int32_t *counts, int32_t *new_lens, void *stream);
+
+/*
  * Testing aids (they follow no passage of the paper; process-wide, not meant for production).
  *
  * mom_debug_force_gemm_form: every later matrix-core launch uses tiles of tile_edge token rows and

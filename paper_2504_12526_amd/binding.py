@@ -21,10 +21,13 @@ SYMBOLS = ("mom_status_string", "mom_mlp_workspace_bytes", "mom_mlp_prefill", "m
            "mom_mlp_prefill_static",
            "mom_debug_mfma_probe",
            "mom_mx_block_bytes", "mom_mx_kv_append", "mom_mx_kv_read", "mom_mx_attention_workspace_bytes", "mom_mx_attention",
-           "mom_mx_quantize", "mom_mx_matvec", "mom_mx_gateup")
+           "mom_mx_quantize", "mom_mx_matvec", "mom_mx_gateup",
+           "mom_mx_tree", "mom_mx_tree_attention_workspace_bytes", "mom_mx_tree_attention", "mom_verify_drafts_workspace_bytes", "mom_verify_drafts",
+           "mom_mx_kv_keep")
 
 MOM_STATIC_WORKSPACE_BYTES = 64 << 20
 MOM_MX_MAX_ROWS = 16
+MOM_MAX_DRAFT_ROWS = 512
 
 (MOM_OK, MOM_ERR_NULL, MOM_ERR_SHAPE, MOM_ERR_ALIGN, MOM_ERR_ALIAS, MOM_ERR_WORKSPACE, MOM_ERR_HIP,
  MOM_ERR_HOST) = range(8)
@@ -100,6 +103,19 @@ def lib():
         L.mom_mx_matvec.argtypes = [vp, i64, vp, vp, i64, i64, vp, ctypes.c_int, vp, vp]
         L.mom_mx_gateup.restype = ctypes.c_int
         L.mom_mx_gateup.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, vp, vp]
+        L.mom_mx_tree.restype = ctypes.c_int
+        L.mom_mx_tree.argtypes = [vp, vp, i64, i64, vp, vp, i64, i64, i64, vp, i64, vp, vp, vp]
+        L.mom_mx_tree_attention_workspace_bytes.restype = sz
+        L.mom_mx_tree_attention_workspace_bytes.argtypes = [i64] * 6
+        L.mom_mx_tree_attention.restype = ctypes.c_int
+        L.mom_mx_tree_attention.argtypes = [vp, i64, vp, i64, i64, i64, i64, i64, vp, i64, i64, vp, i64, vp, i64, ctypes.c_float, i64,
+                                            vp, i64, vp, vp, vp, sz, vp]
+        L.mom_verify_drafts_workspace_bytes.restype = sz
+        L.mom_verify_drafts_workspace_bytes.argtypes = [i64] * 3
+        L.mom_verify_drafts.restype = ctypes.c_int
+        L.mom_verify_drafts.argtypes = [vp, i64, vp, i64, ctypes.c_int, i64, vp, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mom_mx_kv_keep.restype = ctypes.c_int
+        L.mom_mx_kv_keep.argtypes = [vp, i64, i64, i64, i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -322,6 +338,15 @@ def _cache(cache, page_tokens, head_dim):
     return cache.shape[0], cache.shape[1]
 
 
+def _table(page_table):
+    """Sequences and pages of each of a page table whose rows may lie apart, and their distance."""
+    B, each = page_table.shape
+    if page_table.dtype != torch.int32 or (each > 1 and page_table.stride(1) != 1) or (B > 1 and page_table.stride(0) < each):
+        raise ValueError("page_table must be an int32 tensor [B, n] with contiguous rows")
+    # rows that lie apart are passed as one that is as long as their distance, and what lies between them stays out of reach through max_kv
+    return B, each, page_table.stride(0) if B > 1 else each
+
+
 def mom_mx_kv_append(k, v, slots, cache, page_tokens, positions=None, inv_freq=None, interleaved=False, q=None, q_out=None,
                      stream=None, check=True):
     """k, v [T, kv_heads, head_dim] bf16 (tokens may lie apart, as slices of one projection do) into the uint8 cache
@@ -375,11 +400,7 @@ def mom_mx_attention(q, cache, page_tokens, page_table, kv_lens, max_kv, out, wo
     lse [T, q_heads] fp32 or None; workspace any device tensor of at least mom_mx_attention_workspace_bytes bytes, or None where that is 0."""
     T, q_heads, d = q.shape
     pages, kv_heads = _cache(cache, page_tokens, d)
-    B, each = page_table.shape
-    if page_table.dtype != torch.int32 or (each > 1 and page_table.stride(1) != 1) or (B > 1 and page_table.stride(0) < each):
-        raise ValueError("page_table must be an int32 tensor [B, n] with contiguous rows")
-    # rows that lie apart are passed as one that is as long as their distance, and what lies between them stays out of reach through max_kv
-    table_stride = page_table.stride(0) if B > 1 else each
+    B, each, table_stride = _table(page_table)
     _dense("kv_lens", kv_lens, torch.int32, (B,))
     if q_starts is not None:
         _dense("q_starts", q_starts, torch.int32, (B + 1,))
@@ -436,4 +457,118 @@ def mom_mx_gateup(x, gate_codes, gate_scales, up_codes, up_scales, out, stream=N
     rc = lib().mom_mx_gateup(_ptr(x), M, _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes), _ptr(up_scales), N, K, _ptr(out), _stream(stream))
     if check and rc != MOM_OK:
         raise MomError(rc, "mom_mx_gateup")
+    return rc
+
+
+def _starts(q_starts, T, B):
+    if q_starts is not None:
+        _dense("q_starts", q_starts, torch.int32, (B + 1,))
+    elif B == 0 or T % B:
+        raise ValueError("without q_starts every sequence has the same number of rows")
+
+
+def mom_mx_tree(kv_lens, parents=None, q_starts=None, masks=None, positions=None, slots=None, page_table=None, page_tokens=0, stream=None, check=True):
+    """Trees of drafted rows as the other calls take them: kv_lens [B] int32, parents [T] int32 (None: chains), q_starts [B + 1] int32 or None.  Outputs, any of them None: masks
+    [T, words] int32, positions [T] int32, slots [T] int64 (with page_table [B, n] int32 and page_tokens)."""
+    outs = [t for t in (masks, positions, slots) if t is not None]
+    if not outs:
+        raise ValueError("there is nothing to be written")
+    T, B = outs[0].shape[0], kv_lens.shape[0]
+    _dense("kv_lens", kv_lens, torch.int32, (B,))
+    _starts(q_starts, T, B)
+    if parents is not None:
+        _dense("parents", parents, torch.int32, (T,))
+    words = 0
+    if masks is not None:
+        words = masks.shape[-1]
+        _dense("masks", masks, torch.int32, (T, words))
+    if positions is not None:
+        _dense("positions", positions, torch.int32, (T,))
+    each = table_stride = 0
+    if slots is not None:
+        _dense("slots", slots, torch.int64, (T,))
+        sequences, each, table_stride = _table(page_table)
+        if sequences != B:
+            raise ValueError("page_table must have a row for every sequence")
+    rc = lib().mom_mx_tree(_ptr(parents), _ptr(q_starts), T, B, _ptr(kv_lens), _ptr(page_table if slots is not None else None), table_stride, int(page_tokens),
+                           each * int(page_tokens), _ptr(masks), words, _ptr(positions), _ptr(slots), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_tree")
+    return rc
+
+
+def mom_mx_tree_attention_workspace_bytes(T, B, q_heads, kv_heads, head_dim, max_kv):
+    return int(lib().mom_mx_tree_attention_workspace_bytes(int(T), int(B), int(q_heads), int(kv_heads), int(head_dim), int(max_kv)))
+
+
+def mom_mx_tree_attention(q, cache, page_tokens, page_table, kv_lens, max_kv, masks, out, workspace, q_starts=None, scale=None, window=0, lse=None,
+                          stream=None, check=True):
+    """mom_mx_attention of rows of trees: masks [T, words] int32 as mom_mx_tree writes them, workspace of mom_mx_tree_attention_workspace_bytes."""
+    T, q_heads, d = q.shape
+    pages, kv_heads = _cache(cache, page_tokens, d)
+    B, each, table_stride = _table(page_table)
+    _dense("kv_lens", kv_lens, torch.int32, (B,))
+    if q_starts is not None:
+        _dense("q_starts", q_starts, torch.int32, (B + 1,))
+    _dense("masks", masks, torch.int32, (T, masks.shape[-1]))
+    _dense("out", out, torch.bfloat16, q.shape)
+    if lse is not None:
+        _dense("lse", lse, torch.float32, (T, q_heads))
+    rc = lib().mom_mx_tree_attention(_ptr(q), _tokens("q", q), _ptr(q_starts), T, B, q_heads, kv_heads, d, _ptr(cache), pages, int(page_tokens),
+                                     _ptr(page_table), table_stride, _ptr(kv_lens), min(int(max_kv), each * int(page_tokens)),
+                                     1.0 / math.sqrt(d) if scale is None else float(scale), int(window), _ptr(masks), masks.shape[-1], _ptr(out), _ptr(lse),
+                                     _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_tree_attention")
+    return rc
+
+
+def _logits(name, t, dtype=None, shape=None):
+    """[T, V] fp32 or bf16 whose rows may lie apart; the elements between two of them."""
+    if t.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and t.dtype != dtype) or t.dim() != 2 or (shape is not None and t.shape != shape) or \
+            (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name} must be a float32 or bfloat16 tensor [rows, vocabulary] with contiguous rows, target and draft alike")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def mom_verify_drafts_workspace_bytes(T, B, V):
+    return int(lib().mom_verify_drafts_workspace_bytes(int(T), int(B), int(V)))
+
+
+def mom_verify_drafts(target, tokens, uniforms, rows, out_tokens, counts, workspace, draft=None, parents=None, max_children=1, q_starts=None, temperatures=None,
+                      stream=None, check=True):
+    """Which of the drafted tokens [T] int32 stay: target and draft [T, V] logits (rows may lie apart), uniforms [T] fp32, parents [T] int32 (None: chains), temperatures [B] fp32
+    (None: 1).  rows, out_tokens [T] and counts [B] int32 out; workspace any device tensor of at least mom_verify_drafts_workspace_bytes bytes."""
+    T, V = target.shape
+    B = counts.shape[0]
+    target_stride = _logits("target", target)
+    draft_stride = 0 if draft is None else _logits("draft", draft, target.dtype, target.shape)
+    for name, t in (("tokens", tokens), ("rows", rows), ("out_tokens", out_tokens)) + ((("parents", parents),) if parents is not None else ()):
+        _dense(name, t, torch.int32, (T,))
+    _dense("uniforms", uniforms, torch.float32, (T,))
+    _dense("counts", counts, torch.int32, (B,))
+    _starts(q_starts, T, B)
+    if temperatures is not None:
+        _dense("temperatures", temperatures, torch.float32, (B,))
+    rc = lib().mom_verify_drafts(_ptr(target), target_stride, _ptr(draft), draft_stride, int(target.dtype == torch.bfloat16), V, _ptr(tokens), _ptr(parents), int(max_children),
+                                 _ptr(q_starts), T, B, _ptr(temperatures), _ptr(uniforms), _ptr(rows), _ptr(out_tokens), _ptr(counts), _ptr(workspace), _nbytes(workspace),
+                                 _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_verify_drafts")
+    return rc
+
+
+def mom_mx_kv_keep(cache, page_tokens, head_dim, page_table, kv_lens, rows, counts, new_lens, q_starts=None, stream=None, check=True):
+    """The rows [T] int32 that stay, counts [B] int32 of each sequence, moved together in the cache; new_lens [B] int32 out."""
+    pages, kv_heads = _cache(cache, page_tokens, head_dim)
+    B, each, table_stride = _table(page_table)
+    T = rows.shape[0]
+    _dense("rows", rows, torch.int32, (T,))
+    for name, t in (("kv_lens", kv_lens), ("counts", counts), ("new_lens", new_lens)):
+        _dense(name, t, torch.int32, (B,))
+    _starts(q_starts, T, B)
+    rc = lib().mom_mx_kv_keep(_ptr(cache), pages, int(page_tokens), kv_heads, int(head_dim), _ptr(page_table), table_stride, each * int(page_tokens), _ptr(kv_lens),
+                              _ptr(q_starts), T, B, _ptr(rows), _ptr(counts), _ptr(new_lens), _stream(stream))
+    if check and rc != MOM_OK:
+        raise MomError(rc, "mom_mx_kv_keep")
     return rc

@@ -24,9 +24,11 @@
 #include "mom_kv.hip.inc"
 #include "mom_probe.hip.inc"
 #include "mom_mx.h"
+#include "mom_draft.h"
 #include "mom_mx_kv.hip.inc"
 #include "mom_mx_attention.hip.inc"
 #include "mom_mx_matvec.hip.inc"
+#include "mom_draft.hip.inc"
 
 // Workspace of mom_mlp_prefill_static: one copy per device, held from the moment the library is
 // loaded on a device until the process ends.  In host code this name is only a handle for
@@ -683,3 +685,4 @@ int mom_kv_reload(const void* pinned_host, void* k, void* v, void* stream, size_
 }  // extern "C"
 
 #include "mom_mx_calls.hip.inc"
+#include "mom_draft_calls.hip.inc"

@@ -1,0 +1,143 @@
+// Drafted tokens in a tree: what a row sees, how the logits are cut into chunks and where their sums lie, and the power of two in 64 bits, as kernels
+// (mom_draft.hip.inc, mom_mx_attention.hip.inc), entry points and a host program (tests/draft_check.cpp) ask.  Plain C++17, no HIP types.
+//
+// The rows of a sequence are its m new tokens: row i is token n - m + i of the n in the cache.  Bit j of a row's mask says that it sees row j.
+#ifndef MOM_DRAFT_H
+#define MOM_DRAFT_H
+
+#include <math.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "mom_mx.h"
+
+namespace momk {
+namespace draft {
+
+constexpr int kMostRows = 512;                          // rows of a sequence that masks and verification know
+constexpr int kMostWords = kMostRows / 32;
+
+// ---- what a row sees ------------------------------------------------------------------------------------------------------
+
+// The row above row j by the list of parents (null: a chain); -1 where there is none, which what is no earlier row says too.
+MOM_MX_FN int above(const int32_t* parents, int j) {
+    const int p = parents ? parents[j] : j - 1;
+    return p >= 0 && p < j ? p : -1;
+}
+
+// Bits [lo, hi) of 32, the bounds being any numbers.
+MOM_MX_FN uint32_t bits_between(int lo, int hi) {
+    if (lo < 0) lo = 0;
+    if (hi > 32) hi = 32;
+    if (hi <= lo) return 0;
+    return (0xffffffffu >> (32 - (hi - lo))) << lo;
+}
+
+// The 32 bits of a mask of `words` words from bit j on, which may lie outside of it.
+MOM_MX_FN uint32_t mask_bits(const uint32_t* mask, int words, int j) {
+    const int w = j >> 5, s = j & 31;
+    const uint32_t low = w >= 0 && w < words ? mask[w] : 0, high = s && w + 1 >= 0 && w + 1 < words ? mask[w + 1] : 0;
+    return s ? low >> s | high << (32 - s) : low;
+}
+
+// With a window a row sees the last `window` (over 0) of what its mask and the tokens before the m rows give it, in the order of the cache: tokens
+// [from, base) of those, base = n - m, and of its mask the bits from `first` on.
+struct Sight { int from, first; };
+MOM_MX_FN Sight sight(const uint32_t* mask, int words, int base, int m, int window) {
+    const int lowest = base < 0 ? -base : 0, highest = m < 32 * words ? m : 32 * words;
+    if (window <= 0) return {0, lowest};
+    int left = window;
+    for (int w = (highest - 1) >> 5; w >= 0 && 32 * w + 32 > lowest; --w) {
+        uint32_t x = mask[w] & bits_between(lowest - 32 * w, highest - 32 * w);
+        const int count = __builtin_popcount(x);
+        if (count >= left) {
+            for (int i = left; i < count; ++i) x &= x - 1;
+            return {base, 32 * w + __builtin_ctz(x)};
+        }
+        left -= count;
+    }
+    return {base > left ? base - left : 0, lowest};
+}
+
+// The tokens that any row of a sequence sees: what its window leaves of those before the rows (a row without bits has the most of them), and the rows.
+MOM_MX_FN mx::Span tree_span(int n, int m, int window) {
+    const int lo = window > 0 && n - m > window ? n - m - window : 0;
+    if (n <= lo) return {0, 0};
+    return {lo, n};
+}
+// The tokens that all rows see and no mask has a say in: [lo, hi).
+MOM_MX_FN mx::Span tree_whole(int n, int m, int window) {
+    const int base = n - m;
+    int lo = window > 0 ? base - window + (m < window ? m : window) : 0;
+    if (lo < 0) lo = 0;
+    return {lo, base > 0 ? base : 0};
+}
+// Tokens that a tile can reach (mx::tile_reach of a chain): `rows` of a sequence at most.
+MOM_MX_FN int64_t tree_reach(int64_t max_kv, int64_t window, int64_t rows) {
+    if (window <= 0) return max_kv;
+    const int64_t r = window + rows + mx::kStep;
+    return r < max_kv ? r : max_kv;
+}
+
+// How a call is launched, and its workspace: as attention of a chain is, but for the reach.
+MOM_MX_FN mx::AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window, bool listed) {
+    return mx::attention_plan(T, B, Hq, Hkv, D, tree_reach(max_kv, window, listed ? T : T / B), 0, listed);
+}
+MOM_MX_FN size_t tree_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) { return mx::attention_workspace(T, B, Hq, Hkv, D, max_kv); }
+
+// ---- verification ---------------------------------------------------------------------------------------------------------
+
+// 2^t in 64 bits for t <= 0: t = n + f with |f| <= 1/2, Taylor's sum of 2^f = e^(f ln 2) to f^10 (the next term is under 2.2e-13 of it), and n as the exponent.  Whatever is under
+// 2^-1074 is 0, minus infinity among it.
+MOM_MX_FN double power_of_two(double t) {
+    t = t > -1100.0 ? t : -1100.0;                      // (NaN too)
+    const double n = rint(t), f = t - n;
+    constexpr double kLn2 = 0.69314718055994530942;
+    constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4, c5 = c4 * kLn2 / 5, c6 = c5 * kLn2 / 6, c7 = c6 * kLn2 / 7, c8 = c7 * kLn2 / 8,
+                     c9 = c8 * kLn2 / 9, c10 = c9 * kLn2 / 10;
+    double y = fma(c10, f, c9);
+    y = fma(y, f, c8);
+    y = fma(y, f, c7);
+    y = fma(y, f, c6);
+    y = fma(y, f, c5);
+    y = fma(y, f, c4);
+    y = fma(y, f, c3);
+    y = fma(y, f, c2);
+    y = fma(y, f, c1);
+    y = fma(y, f, 1.0);
+    return ldexp(y, (int)n);
+}
+
+constexpr int kChunk = 4096;                            // logits of a row that a workgroup sums at once
+constexpr int64_t kMostVocabulary = (int64_t)1 << 30;
+MOM_MX_FN int64_t chunks(int64_t V) { return (V + kChunk - 1) / kChunk; }
+
+// What lies in the workspace of a verification: sums of the chunks of each row of both models and of what is left there, then what is known of a row.
+struct Part { double sum; float most; int32_t place; };                 // of a chunk: its largest logit and that one's place, sum of 2^((l - most) k)
+struct Row {
+    double target_top, target_inverse;                  // probabilities of the target here: 2^((l - top) k) inverse
+    double draft_top, draft_inverse;
+    double p, q;                                        // probabilities of this row's token at the row above
+    double cut, rest;                                   // what is left here is max(p - cut q, 0) / rest
+    int32_t rank, verdict, place, left;                 // which child it is; kOpen ...; the target's largest logit; refused children that `cut` counts
+    int32_t again, unused;                              // an earlier child of the same row is the same token
+};
+constexpr int kOpen = 0, kTaken = 1, kRefused = 2, kPassed = 3;         // kPassed: not tried
+struct Layout { size_t target, draft, rest, rows, lists, bytes; };
+MOM_MX_FN Layout layout(int64_t T, int64_t B, int64_t V) {
+    const size_t cells = (size_t)T * (size_t)chunks(V);
+    Layout l;
+    l.target = 0;
+    l.draft = l.target + cells * sizeof(Part);
+    l.rest = l.draft + cells * sizeof(Part);
+    l.rows = l.rest + cells * sizeof(double);
+    l.lists = l.rows + (size_t)T * sizeof(Row);
+    l.bytes = l.lists + (size_t)(T + B) * sizeof(int32_t);
+    l.bytes = (l.bytes + 15) / 16 * 16;
+    return l;
+}
+
+}  // namespace draft
+}  // namespace momk
+
+#endif
