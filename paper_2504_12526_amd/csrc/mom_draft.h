@@ -120,7 +120,7 @@ struct Row {
     double p, q;                                        // probabilities of this row's token at the row above
     double cut, rest;                                   // what is left here is max(p - cut q, 0) / rest
     int32_t rank, verdict, place, left;                 // which child it is; kOpen ...; the target's largest logit; refused children that `cut` counts
-    int32_t again, unused;                              // an earlier child of the same row is the same token
+    int32_t again, held;                                // an earlier child of the same row is the same token; where a workgroup has its chunks' rests
 };
 constexpr int kOpen = 0, kTaken = 1, kRefused = 2, kPassed = 3;         // kPassed: not tried
 struct Layout { size_t target, draft, rest, rows, lists, bytes; };
@@ -130,9 +130,9 @@ MOM_MX_FN Layout layout(int64_t T, int64_t B, int64_t V) {
     l.target = 0;
     l.draft = l.target + cells * sizeof(Part);
     l.rest = l.draft + cells * sizeof(Part);
-    l.rows = l.rest + cells * sizeof(double);
-    l.lists = l.rows + (size_t)T * sizeof(Row);
-    l.bytes = l.lists + (size_t)(T + B) * sizeof(int32_t);
+    l.rows = l.rest + 2 * cells * sizeof(double);
+    l.lists = l.rows + 2 * (size_t)T * sizeof(Row);
+    l.bytes = l.lists + 2 * (size_t)(T + B) * sizeof(int32_t);
     l.bytes = (l.bytes + 15) / 16 * 16;
     return l;
 }

@@ -125,7 +125,7 @@ static void check_layout() {
         CHECK(draft::chunks(V) * draft::kChunk >= V && (draft::chunks(V) - 1) * draft::kChunk < V, "chunks of %d", (int)V);
         const draft::Layout l = draft::layout(T, B, V);
         const size_t ends[] = {l.target, l.draft, l.rest, l.rows, l.lists, l.bytes};
-        const size_t sizes[] = {(size_t)cells * sizeof(draft::Part), (size_t)cells * sizeof(draft::Part), (size_t)cells * 8, (size_t)T * sizeof(draft::Row), (size_t)(T + B) * 4};
+        const size_t sizes[] = {(size_t)cells * sizeof(draft::Part), (size_t)cells * sizeof(draft::Part), 2 * (size_t)cells * 8, 2 * (size_t)T * sizeof(draft::Row), 2 * (size_t)(T + B) * 4};
         for (int i = 0; i < 5; ++i) CHECK(ends[i] % (i < 4 ? 8 : 4) == 0 && ends[i] + sizes[i] <= ends[i + 1], "layout part %d", i);
         CHECK(l.target % 16 == 0 && l.draft % 16 == 0 && l.bytes % 16 == 0, "layout");
     }

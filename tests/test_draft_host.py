@@ -48,7 +48,7 @@ def test_what_rows_see_shares_powers_and_workspaces(tmp_path):
     ("c10 = c9 * kLn2 / 10;", "c10 = 0;", "power"),
     ("t = t > -1100.0 ? t : -1100.0;", "", "power"),
     ("{ return (V + kChunk - 1) / kChunk; }", "{ return V / kChunk + 1; }", "chunks"),
-    ("l.lists = l.rows + (size_t)T * sizeof(Row);", "l.lists = l.rows + (size_t)T * sizeof(Part);", "layout"),
+    ("l.lists = l.rows + 2 * (size_t)T * sizeof(Row);", "l.lists = l.rows + (size_t)T * sizeof(Row);", "layout"),
 ])
 def test_a_planted_mistake_is_caught(tmp_path, old, new, says):
     """Planted in a copy of the header, on the CPU."""
