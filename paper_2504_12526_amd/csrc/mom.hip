@@ -29,6 +29,7 @@
 #include "mom_mx_attention.hip.inc"
 #include "mom_mx_matvec.hip.inc"
 #include "mom_draft.hip.inc"
+#include "mom_draft_attention.hip.inc"
 
 // Workspace of mom_mlp_prefill_static: one copy per device, held from the moment the library is
 // loaded on a device until the process ends.  In host code this name is only a handle for

@@ -72,18 +72,69 @@ MOM_MX_FN mx::Span tree_whole(int n, int m, int window) {
     if (lo < 0) lo = 0;
     return {lo, base > 0 ? base : 0};
 }
-// Tokens that a tile can reach (mx::tile_reach of a chain): `rows` of a sequence at most.
-MOM_MX_FN int64_t tree_reach(int64_t max_kv, int64_t window, int64_t rows) {
-    if (window <= 0) return max_kv;
-    const int64_t r = window + rows + mx::kStep;
-    return r < max_kv ? r : max_kv;
+// How attention is launched: tiles of 16 qb rows whose tokens `wk` wavefronts share; their tokens in shares, as many as `workgroups` of a key head that there are at once allow
+// (the device knows the lengths); whole: a workgroup a tile, and nothing to join.
+struct AttentionPlan {
+    int qb, wk, rows;
+    bool whole;
+    int64_t numbers, workgroups, tiles;                 // numbers: of tiles of a key head at most; tiles: about as many there are, of all heads
+};
+constexpr int kWholeTokens = 768, kAtOnce = 256;
+MOM_MX_FN AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window, bool listed) {
+    const int group = Hq / Hkv;
+    const int64_t average = (T * group + B - 1) / B, rows = listed ? T : T / B;
+    int64_t reach = max_kv;
+    if (window > 0 && window + rows + mx::kStep < reach) reach = window + rows + mx::kStep;
+    AttentionPlan p;
+    p.wk = 8;
+    p.qb = average <= 16 || D == 256 ? 1 : 2;
+    {
+        p.rows = 16 * p.qb;
+        const int64_t even = B * ((average + p.rows - 1) / p.rows), uneven = (2 * T * group + (B + 1) * p.rows - 1) / (2 * p.rows);
+        p.tiles = (!listed ? even : uneven < B ? B : uneven) * Hkv;
+        p.numbers = listed ? mx::tile_numbers(T, B, group, p.rows) : even;
+        // of all heads as many as the compute units hold at once
+        const int64_t at_once = kAtOnce * (p.qb == 1 && D <= 128 ? 2 : 1);
+        p.workgroups = (at_once + Hkv - 1) / Hkv;
+        p.whole = reach <= kWholeTokens || p.tiles >= p.workgroups * Hkv || p.numbers >= 2 * p.workgroups;
+        return p;
+    }
 }
-
-// How a call is launched, and its workspace: as attention of a chain is, but for the reach.
-MOM_MX_FN mx::AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window, bool listed) {
-    return mx::attention_plan(T, B, Hq, Hkv, D, tree_reach(max_kv, window, listed ? T : T / B), 0, listed);
+// Shares of a tile of `steps` (at least 1, under 2^24) that are no longer than `share`.
+MOM_MX_FN uint32_t shares_of(uint32_t steps, uint32_t share) {
+    uint32_t q = (uint32_t)((float)steps * (1.0f / (float)share));       // two roundings: the quotient cut off, or one less
+    q += q * share < steps;
+    q += q * share < steps;
+    return q < 1 ? 1 : q;
 }
-MOM_MX_FN size_t tree_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) { return mx::attention_workspace(T, B, Hq, Hkv, D, max_kv); }
+// The shortest share, counted in `wk` steps, with which all tiles make no more shares than `workgroups` (or none of them two): sum(f) is the sum of f(x) over all sequences x, x.tiles
+// tiles of x.steps steps, at most `most`.
+struct ShareCount {
+    uint32_t share;
+    template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles * shares_of(x.steps, share); }
+};
+struct StepCount { template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles * x.steps; } };
+struct TileCount { template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles; } };
+template <typename Sum>
+MOM_MX_FN uint32_t shortest_share(uint32_t workgroups, uint32_t most, uint32_t wk, const Sum& sum) {
+    const uint32_t steps = sum(StepCount()), tiles = sum(TileCount());
+    uint32_t lo = (steps / workgroups + wk - 1) / wk, hi = (most + wk) / wk;
+    // a tile makes a share of its own and one for every whole share in it at most: so many steps are enough
+    if (tiles < workgroups && steps / (workgroups - tiles) / wk + 1 < hi) hi = steps / (workgroups - tiles) / wk + 1;
+    if (lo < 1) lo = 1;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (sum(ShareCount{mid * wk}) <= workgroups) hi = mid;
+        else lo = mid + 1;
+    }
+    return hi;
+}
+MOM_MX_FN int64_t plan_workgroups(const AttentionPlan& p) { return p.whole || p.numbers > p.workgroups ? p.numbers : p.workgroups; }
+MOM_MX_FN size_t plan_workspace(const AttentionPlan& p, int Hkv, int D) { return p.whole ? 0 : (size_t)p.workgroups * Hkv * p.rows * (D + 2) * 4; }
+MOM_MX_FN size_t tree_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
+    const size_t even = plan_workspace(tree_plan(T, B, Hq, Hkv, D, max_kv, 0, false), Hkv, D), uneven = plan_workspace(tree_plan(T, B, Hq, Hkv, D, max_kv, 0, true), Hkv, D);
+    return even > uneven ? even : uneven;
+}
 
 // ---- verification ---------------------------------------------------------------------------------------------------------
 

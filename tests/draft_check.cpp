@@ -75,33 +75,63 @@ static void check_sight() {
         for (int t : want) CHECK(t >= span.lo && t < span.hi, "span n %d m %d window %d token %d", n, m, window, t);
         for (int t = whole.lo; t < whole.hi; ++t) CHECK(std::binary_search(want.begin(), want.end(), t), "whole n %d m %d window %d token %d", n, m, window, t);
         CHECK(whole.hi <= std::max(base, 0), "whole");
-        // shares of a plan for this call, or for longer sequences and more rows than there are, cover the span
-        const int64_t most = n + upto(100), rows = m + upto(50), reach = draft::tree_reach(most, window, rows);
-        const int64_t shares = 1 + upto(9), share = ((reach + shares - 1) / shares + mx::kStep - 1) / mx::kStep * mx::kStep;
-        int64_t covered = span.lo;
-        for (int64_t z = 0; z * share < reach; ++z) {
-            const mx::Span p = mx::share_span(span, (int)z, (int)share);
-            if (p.hi > p.lo) {
-                CHECK(p.lo == covered, "shares n %d m %d window %d", n, m, window);
-                covered = p.hi;
+        // shares of any length cover the span, one after the other
+        const int origin = span.lo / mx::kStep * mx::kStep;
+        const uint32_t steps = std::max((span.hi + mx::kStep - 1) / mx::kStep - span.lo / mx::kStep, 1), cut = draft::shares_of(steps, 1 + upto(80)), each = (steps + cut - 1) / cut;
+        int covered = span.lo;
+        for (uint32_t z = 0; z < cut; ++z) {
+            const int lo = std::max(span.lo, origin + (int)(z * each) * mx::kStep), hi = std::max(std::min(span.hi, origin + (int)((z + 1) * each) * mx::kStep), lo);
+            if (hi > lo) {
+                CHECK(lo == covered, "shares n %d m %d window %d", n, m, window);
+                covered = hi;
             }
         }
-        CHECK(covered >= span.hi || span.hi <= span.lo, "shares cover %d of %d, m %d window %d", (int)covered, span.hi, m, window);
+        CHECK(covered == span.hi || span.hi <= span.lo, "shares cover %d of %d, m %d window %d", covered, span.hi, m, window);
     }
 }
 
 static void check_plan() {
+    for (uint32_t share = 1; share < 700; share += 1 + share / 20)
+        for (int k = 0; k < 300; ++k) {
+            const uint32_t steps = k < 100 ? k + 1 : 1 + upto((1 << 24) - 2);
+            CHECK(draft::shares_of(steps, share) == (steps + share - 1) / share, "shares_of %u %u", steps, share);
+        }
+    for (int k = 0; k < 400000; ++k) {
+        const uint32_t share = 3 + upto(6), steps = (1 << 24) - 1 - upto(1 << 20);
+        CHECK(draft::shares_of(steps, share) == (steps + share - 1) / share, "shares_of %u %u", steps, share);
+    }
+    CHECK(draft::shares_of(12345, 1u << 27) == 1, "shares_of");
     for (int k = 0; k < 20000; ++k) {
         const int heads[][2] = {{32, 8}, {28, 4}, {8, 8}, {16, 1}, {16, 4}, {1, 1}};
         const int* h = heads[upto(5)];
-        const int D = 64 << upto(2);
-        const int64_t B = 1 + upto(60), T = B * (1 + upto(upto(1) ? 16 : 300)), max_kv = upto(3) ? upto(9000) : upto(200000), window = upto(2) ? 0 : 1 + upto(5000);
+        const int D = 64 << upto(2), group = h[0] / h[1];
+        const int64_t B = 1 + upto(60), each = 1 + upto(upto(1) ? 16 : 300), max_kv = upto(3) ? upto(9000) : upto(200000), window = upto(2) ? 0 : 1 + upto(5000);
         for (int listed = 0; listed < 2; ++listed) {
-            const mx::AttentionPlan p = draft::tree_plan(T, B, h[0], h[1], D, max_kv, window, listed);
-            const int64_t reach = draft::tree_reach(max_kv, window, listed ? T : T / B);
-            CHECK(p.shares >= 1 && p.share % mx::kStep == 0 && (int64_t)p.shares * p.share >= reach, "plan reach T %d B %d", (int)T, (int)B);
-            const size_t need = p.shares > 1 ? (size_t)p.shares * T * h[0] * (D + 2) * 4 : 0;
-            CHECK(need <= draft::tree_workspace(T, B, h[0], h[1], D, max_kv), "plan workspace T %d B %d heads %d D %d kv %d window %d", (int)T, (int)B, h[0], D, (int)max_kv, (int)window);
+            struct X { uint32_t tiles, steps; };
+            std::vector<int> ms(B);
+            int64_t T = 0;
+            for (auto& m : ms) T += m = listed ? upto((int)each) : (int)each;
+            if (T == 0) continue;
+            const draft::AttentionPlan p = draft::tree_plan(T, B, h[0], h[1], D, max_kv, window, listed);
+            CHECK(p.rows == 16 * p.qb && p.workgroups >= 1, "plan");
+            std::vector<X> xs;
+            uint32_t tiles = 0;
+            for (int m : ms) {
+                const mx::Span s = draft::tree_span(upto((int)max_kv), m, (int)window);
+                xs.push_back({mx::tiles_of(m, group, p.rows), (uint32_t)std::max((s.hi + mx::kStep - 1) / mx::kStep - s.lo / mx::kStep, 1)});
+                tiles += xs.back().tiles;
+            }
+            CHECK(tiles <= p.numbers && tiles <= draft::plan_workgroups(p), "plan numbers T %d B %d", (int)T, (int)B);
+            CHECK(draft::plan_workspace(p, h[1], D) <= draft::tree_workspace(T, B, h[0], h[1], D, max_kv), "plan workspace T %d B %d heads %d D %d kv %d window %d", (int)T, (int)B, h[0], D, (int)max_kv, (int)window);
+            if (p.whole) continue;
+            auto sum = [&](auto of) { uint32_t r = 0; for (const X& x : xs) r += of(x); return r; };
+            const uint32_t share = draft::shortest_share((uint32_t)p.workgroups, (uint32_t)max_kv / mx::kStep + 1, p.wk, sum), count = sum(draft::ShareCount{share * p.wk});
+            bool cut = false, shorter_cuts_less = share > 1 && sum(draft::ShareCount{(share - 1) * p.wk}) <= p.workgroups;
+            for (const X& x : xs) cut |= x.tiles && draft::shares_of(x.steps, share * p.wk) > 1;
+            // what is cut has room in the workspace; nothing shorter would do
+            CHECK(!cut || count <= p.workgroups, "plan share T %d B %d", (int)T, (int)B);
+            CHECK(!cut || draft::plan_workspace(p, h[1], D) >= (size_t)count * h[1] * p.rows * (D + 2) * 4, "plan workspace T %d B %d", (int)T, (int)B);
+            CHECK(count <= draft::plan_workgroups(p) && !shorter_cuts_less, "plan shares T %d B %d: %u of %d, share %u", (int)T, (int)B, count, (int)p.workgroups, share);
         }
     }
 }

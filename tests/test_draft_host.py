@@ -23,7 +23,7 @@ OK, NULL, SHAPE, ALIGN, ALIAS, WORKSPACE = (binding.MOM_OK, binding.MOM_ERR_NULL
 def _check(tmp_path, include):
     exe = os.path.join(str(tmp_path), "draft_check")
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", include, "-o", exe, os.path.join(ROOT, "tests", "draft_check.cpp")], check=True)
-    return subprocess.run([exe], capture_output=True, text=True)
+    return subprocess.run([exe], capture_output=True, text=True, timeout=60)
 
 
 def test_what_rows_see_shares_powers_and_workspaces(tmp_path):
@@ -43,7 +43,9 @@ def test_what_rows_see_shares_powers_and_workspaces(tmp_path):
     ("return {base > left ? base - left : 0, lowest};", "return {0, lowest};", "sight"),
     ("n - m > window ? n - m - window : 0;", "n - m > window ? n - m - window + 1 : 0;", "span"),
     ("base - window + (m < window ? m : window) : 0;", "base - window : 0;", "whole"),
-    ("const int64_t r = window + rows + mx::kStep;", "const int64_t r = window;", "share"),
+    ("    q += q * share < steps;\n    q += q * share < steps;\n", "", "shares"),
+    ("<= workgroups) hi = mid;", "<= 2 * workgroups) hi = mid;", "plan share"),
+    ("(size_t)p.workgroups * Hkv * p.rows", "(size_t)p.numbers * Hkv * p.rows", "plan"),
     ("y = fma(y, f, c3);", "", "power"),
     ("c10 = c9 * kLn2 / 10;", "c10 = 0;", "power"),
     ("t = t > -1100.0 ? t : -1100.0;", "", "power"),
