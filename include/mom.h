@@ -370,7 +370,7 @@ int mom_mx_tree_attention(const void *q, int64_t q_stride, const int32_t *q_star
  *   draft        [T][V] the drafting model's logits at the same rows, same type, draft_stride apart, read where a row has children; NULL: drafts without
  *                probabilities, q(x) = 1 (r loses the refused token alone)
  *   tokens       [T] each row's token; that of row 0 is not looked at
- *   max_children children of a row that are tried, at least 1; more than there are cost two launches each where `draft` is given
+ *   max_children children of a row that are tried, at least 1; more than there are cost a launch each where `draft` is given
  *   temperatures [B] device, t of each sequence, NULL: 1; not above 0: greedy, a child is taken if it is the target's largest logit, which is the next token too
  *   uniforms     [T] numbers in [0, 1): those of rows 1 ... for their drafts, that of row 0 for the next token
  *   rows         [T] out: per sequence from its first row on, the rows that stay: row 0, and down the tree

@@ -79,7 +79,13 @@ struct AttentionPlan {
     bool whole;
     int64_t numbers, workgroups, tiles;                 // numbers: of tiles of a key head at most; tiles: about as many there are, of all heads
 };
-constexpr int kWholeTokens = 768, kAtOnce = 256;
+// Tiles of 16 rows where a sequence has no more, and where all of them together have little to do: a tile of 32 takes longer to begin and to end (8 rows of 32 heads, 8 of them key heads,
+// after 317 tokens 7.1 us, 9.0 with 32; after 1536 12.1 and 13.8; of 64 tiles of 16 rows 24.0, 32.5), but turns the tokens into operands once for twice the rows (32 sequences of 4608 tokens
+// 34.7 us, 46.1 with 16; 16 rows after 131072 59.6 and 88.1; of 128 tiles and 1024 tokens 16.8 and 17.2).  256 dimensions leave registers for 16.
+constexpr int64_t kLittle = 65536;                      // tokens, of all tiles of 16 rows
+// Whole tiles: a second launch joins shares, 5 us.  8 tiles of 32 rows and 1024 tokens take 12.7 us whole and 13.5 in shares, 1536 tokens 15.5 and 13.8; 64 tiles of 1024 12.9 and 16.9; as many tiles
+// as workgroups at once, of lengths up to 8192, 50.6 and 57.7.
+constexpr int kWholeTokens = 1024, kManyWholeTokens = 1536, kManyTiles = 64, kAtOnce = 256;
 MOM_MX_FN AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window, bool listed) {
     const int group = Hq / Hkv;
     const int64_t average = (T * group + B - 1) / B, rows = listed ? T : T / B;
@@ -87,18 +93,16 @@ MOM_MX_FN AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, 
     if (window > 0 && window + rows + mx::kStep < reach) reach = window + rows + mx::kStep;
     AttentionPlan p;
     p.wk = 8;
-    p.qb = average <= 16 || D == 256 ? 1 : 2;
-    {
-        p.rows = 16 * p.qb;
-        const int64_t even = B * ((average + p.rows - 1) / p.rows), uneven = (2 * T * group + (B + 1) * p.rows - 1) / (2 * p.rows);
-        p.tiles = (!listed ? even : uneven < B ? B : uneven) * Hkv;
-        p.numbers = listed ? mx::tile_numbers(T, B, group, p.rows) : even;
-        // of all heads as many as the compute units hold at once
-        const int64_t at_once = kAtOnce * (p.qb == 1 && D <= 128 ? 2 : 1);
-        p.workgroups = (at_once + Hkv - 1) / Hkv;
-        p.whole = reach <= kWholeTokens || p.tiles >= p.workgroups * Hkv || p.numbers >= 2 * p.workgroups;
-        return p;
-    }
+    p.qb = average <= 16 || D == 256 || (average + 15) / 16 * B * Hkv * reach <= kLittle ? 1 : 2;
+    p.rows = 16 * p.qb;
+    const int64_t even = B * ((average + p.rows - 1) / p.rows), uneven = (2 * T * group + (B + 1) * p.rows - 1) / (2 * p.rows);
+    p.tiles = (!listed ? even : uneven < B ? B : uneven) * Hkv;
+    p.numbers = listed ? mx::tile_numbers(T, B, group, p.rows) : even;
+    // of all heads as many as the compute units hold at once
+    const int64_t at_once = kAtOnce * (p.qb == 1 && D <= 128 ? 2 : 1);
+    p.workgroups = (at_once + Hkv - 1) / Hkv;
+    p.whole = reach <= (p.tiles >= kManyTiles ? kManyWholeTokens : kWholeTokens) || p.tiles >= p.workgroups * Hkv || p.numbers >= 2 * p.workgroups;
+    return p;
 }
 // Shares of a tile of `steps` (at least 1, under 2^24) that are no longer than `share`.
 MOM_MX_FN uint32_t shares_of(uint32_t steps, uint32_t share) {
@@ -131,6 +135,7 @@ MOM_MX_FN uint32_t shortest_share(uint32_t workgroups, uint32_t most, uint32_t w
 }
 MOM_MX_FN int64_t plan_workgroups(const AttentionPlan& p) { return p.whole || p.numbers > p.workgroups ? p.numbers : p.workgroups; }
 MOM_MX_FN size_t plan_workspace(const AttentionPlan& p, int Hkv, int D) { return p.whole ? 0 : (size_t)p.workgroups * Hkv * p.rows * (D + 2) * 4; }
+// (Fewer tokens or a window may have tiles of 16 rows where more have 32: twice the workgroups, half the rows, and the same bytes.)
 MOM_MX_FN size_t tree_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
     const size_t even = plan_workspace(tree_plan(T, B, Hq, Hkv, D, max_kv, 0, false), Hkv, D), uneven = plan_workspace(tree_plan(T, B, Hq, Hkv, D, max_kv, 0, true), Hkv, D);
     return even > uneven ? even : uneven;

@@ -209,6 +209,30 @@ def test_attention_with_rows_of_no_sequence_strided_queries_and_pages_that_are_n
     _check(q, cache, 16, table, lens, starts, masks, heads=4, max_kv=70, scale=0.0)
 
 
+@pytest.mark.parametrize("kv,Hkv", [(1700, 1), (1700, 8), (300, 4)])
+def test_attention_of_more_sequences_than_a_wavefront_has_lanes(kv, Hkv):
+    """Most of them short, some without rows, a few long and in shares."""
+    rng = random.Random(7)
+    counts = [rng.choice([0, 1, 3]) for _ in range(150)]
+    lens = [m + rng.randrange(0, 20) for m in counts]
+    for b in (0, 63, 64, 149):
+        counts[b], lens[b] = 5, kv - b
+    q, cache, table, lens, starts = _attend_case(counts, Hkv, Hkv, 64, 16, lens, 16)
+    _check(q, cache, 16, table, lens, starts, _masks(rng, counts, "tree", 1))
+
+
+def test_nan_in_shares():
+    rng, D, P, n, m = random.Random(8), 64, 16, 2600, 7
+    q, cache, table, lens, starts = _attend_case([m], 2, 1, D, P, [n], 17)
+    bad = torch.ones(1, 1, D, dtype=torch.float64)
+    bad[:, :, 32:] = math.nan
+    for j in (n - m + 2, 700):
+        slot = int(table[0, j // P]) * P + j % P
+        cache = ref.append(cache, P, torch.ones(1, 1, D, dtype=torch.float64), bad, torch.tensor([slot]))
+        out, _ = _check(q, cache, P, table, lens, starts, _masks(rng, [m], "tree", 1))
+        assert out[:, :, 32:].isnan().any() and not out[:, :, :32].isnan().any()
+
+
 @pytest.mark.parametrize("m", [6, 72])
 def test_attention_of_sequences_with_as_many_rows_each(m):
     q, cache, table, lens, _ = _attend_case([m] * 3, 4, 1, 128, 16, [m, m + 40, m + 17], 13)
@@ -328,6 +352,39 @@ def test_verify_chains(B, m, V, draft):
     if m > binding.MOM_MAX_DRAFT_ROWS:
         assert max(want[2]) == binding.MOM_MAX_DRAFT_ROWS or not draft   # the way down ends where the rows are not known any more
     _same(got, want)
+
+
+def test_verify_of_more_sequences_than_a_wavefront_has_lanes():
+    gen, rng, V = _gen(18), random.Random(18), 300
+    counts = [rng.choice([0, 1, 2, 6]) for _ in range(200)]
+    T, B, starts = 3 + sum(counts) + 1, len(counts), _ints(_starts(counts, 3))
+    parents = _ints(_parents(rng, counts, 2, 3, 1))
+    for draft in (True, False):
+        target, other = _logits(gen, T, V, False, draft)
+        t = torch.tensor([0.0 if b % 7 == 3 else 0.5 + b / B for b in range(B)])
+        tokens = _draws(gen, parents, starts, other, target, T, V, t.tolist())
+        uniforms = torch.rand(T, generator=gen)
+        _same(_verify(target, tokens, uniforms, B, other, parents, 3, starts, t), dref.verify(target, other, tokens, parents, 3, starts, t, uniforms))
+
+
+def test_verify_of_logits_far_from_the_first():
+    """Sums are relative to a row's first logit: far above it, far below it, infinite, and large ones whose products are rounded."""
+    gen, V, B = _gen(19), 9001, 8
+    target, other = _logits(gen, 2 * B, V, False, True)
+    for x in (target, other):
+        x[0:2, 0] = 2000.0
+        x[2:4, 0] = -2000.0
+        x[4:6, 0] = -math.inf
+        x[6:8] *= 1e6
+        x[8:10, 4096:] = -math.inf
+        x[10:12] += 5e4
+        x[12:14, 0], x[12:14, 5000] = math.nan, math.inf
+        x[14:16, :8999] = -math.inf
+    tokens, uniforms = torch.randint(0, V, (2 * B,), generator=gen).to(torch.int32), torch.rand(2 * B, generator=gen)
+    tokens[1], tokens[7], tokens[13], tokens[15] = 0, int(target[6].argmax()), 5000, 9000
+    for t in (None, torch.full((B,), 0.01), torch.full((B,), 300.0), torch.full((B,), math.inf)):
+        for draft in (other, None):
+            _same(_verify(target, tokens, uniforms, B, draft, None, 1, None, t), dref.verify(target, draft, tokens, None, 1, [2 * b for b in range(B + 1)], t, uniforms))
 
 
 def test_verify_of_a_star_with_many_children():
