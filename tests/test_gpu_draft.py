@@ -273,6 +273,24 @@ def test_chains_are_those_of_the_other_call(counts, lens):
     _within(other, want, err)
 
 
+def test_attention_and_slots_by_a_table_whose_rows_lie_apart():
+    counts, lens, P, D = [6, 40, 3], [100, 90, 33], 16, 64
+    q, cache, table, lens, starts = _attend_case(counts, 2, 1, D, P, lens, 18)
+    masks = _masks(random.Random(9), counts, "tree", 2)
+    wide = torch.full((3, table.shape[1] + 5), -7, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    apart = wide.to(DEV)[:, :table.shape[1]]
+    out, other = (torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    args = dict(q_starts=starts.to(DEV))
+    for t, o in ((apart, out), (table.to(DEV), other)):
+        binding.mom_mx_tree_attention(q.to(DEV), cache.to(DEV), P, t, lens.to(DEV), 112, masks.to(DEV), o, None, **args)
+    assert torch.equal(out.view(torch.int16), other.view(torch.int16)) and not (out == 7).all()
+    slots = [torch.empty(49, dtype=torch.int64, device=DEV) for _ in range(2)]
+    for t, o in ((apart, slots[0]), (table.to(DEV), slots[1])):
+        binding.mom_mx_tree(lens.to(DEV), slots=o, page_table=t, page_tokens=P, **args)
+    assert torch.equal(*slots) and slots[0].min() >= 0
+
+
 # Verification
 
 def _logits(gen, T, V, bf16, draft, spread=2.0):
@@ -385,6 +403,21 @@ def test_verify_of_logits_far_from_the_first():
     for t in (None, torch.full((B,), 0.01), torch.full((B,), 300.0), torch.full((B,), math.inf)):
         for draft in (other, None):
             _same(_verify(target, tokens, uniforms, B, draft, None, 1, None, t), dref.verify(target, draft, tokens, None, 1, [2 * b for b in range(B + 1)], t, uniforms))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_verify_of_trees_of_as_many_rows_whose_logits_lie_apart(bf16):
+    gen, rng, V, B, m = _gen(21), random.Random(21), 9999, 5, 11
+    T = B * m
+    parents = _ints(_parents(rng, [m] * B, 3))
+    target, other = _logits(gen, T, V, bf16, True)
+    wide = [torch.zeros((T, V + k), dtype=t.dtype) for t, k in ((target, 7), (other, 1))]
+    for w, t in zip(wide, (target, other)):
+        w[:, :V] = t
+    starts = [b * m for b in range(B + 1)]
+    tokens, uniforms = _draws(gen, parents, starts, other, target, T, V, [1.0] * B), torch.rand(T, generator=gen)
+    got = _verify(wide[0][:, :V], tokens, uniforms, B, wide[1][:, :V], parents, 3)
+    _same(got, dref.verify(target, other, tokens, parents, 3, starts, None, uniforms))
 
 
 def test_verify_of_a_star_with_many_children():
