@@ -460,6 +460,15 @@ def mom_mx_gateup(x, gate_codes, gate_scales, up_codes, up_scales, out, stream=N
     return rc
 
 
+def _int32(shape, **tensors):
+    """Dense int32 tensors of one shape, or None (asked all together: a small kernel takes less time than a dozen questions one by one)."""
+    for t in tensors.values():
+        if t is not None and not (t.dtype is torch.int32 and t.shape == shape and t.is_contiguous()):
+            for name, x in tensors.items():
+                if x is not None:
+                    _dense(name, x, torch.int32, shape)
+
+
 def _starts(q_starts, T, B):
     if q_starts is not None:
         _dense("q_starts", q_starts, torch.int32, (B + 1,))
@@ -525,10 +534,11 @@ def mom_mx_tree_attention(q, cache, page_tokens, page_table, kv_lens, max_kv, ma
 
 def _logits(name, t, dtype=None, shape=None):
     """[T, V] fp32 or bf16 whose rows may lie apart; the elements between two of them."""
-    if t.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and t.dtype != dtype) or t.dim() != 2 or (shape is not None and t.shape != shape) or \
-            (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    kind, extents, apart = t.dtype, t.shape, t.stride()
+    if kind not in (torch.float32, torch.bfloat16) or (dtype is not None and kind != dtype) or len(extents) != 2 or (shape is not None and extents != shape) or \
+            (extents[1] > 1 and apart[1] != 1) or (extents[0] > 1 and apart[0] < extents[1]):
         raise ValueError(f"{name} must be a float32 or bfloat16 tensor [rows, vocabulary] with contiguous rows, target and draft alike")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return apart[0] if extents[0] > 1 else extents[1]
 
 
 def mom_verify_drafts_workspace_bytes(T, B, V):
@@ -543,8 +553,7 @@ def mom_verify_drafts(target, tokens, uniforms, rows, out_tokens, counts, worksp
     B = counts.shape[0]
     target_stride = _logits("target", target)
     draft_stride = 0 if draft is None else _logits("draft", draft, target.dtype, target.shape)
-    for name, t in (("tokens", tokens), ("rows", rows), ("out_tokens", out_tokens)) + ((("parents", parents),) if parents is not None else ()):
-        _dense(name, t, torch.int32, (T,))
+    _int32((T,), tokens=tokens, rows=rows, out_tokens=out_tokens, parents=parents)
     _dense("uniforms", uniforms, torch.float32, (T,))
     _dense("counts", counts, torch.int32, (B,))
     _starts(q_starts, T, B)
@@ -564,8 +573,7 @@ def mom_mx_kv_keep(cache, page_tokens, head_dim, page_table, kv_lens, rows, coun
     B, each, table_stride = _table(page_table)
     T = rows.shape[0]
     _dense("rows", rows, torch.int32, (T,))
-    for name, t in (("kv_lens", kv_lens), ("counts", counts), ("new_lens", new_lens)):
-        _dense(name, t, torch.int32, (B,))
+    _int32((B,), kv_lens=kv_lens, counts=counts, new_lens=new_lens)
     _starts(q_starts, T, B)
     rc = lib().mom_mx_kv_keep(_ptr(cache), pages, int(page_tokens), kv_heads, int(head_dim), _ptr(page_table), table_stride, each * int(page_tokens), _ptr(kv_lens),
                               _ptr(q_starts), T, B, _ptr(rows), _ptr(counts), _ptr(new_lens), _stream(stream))
