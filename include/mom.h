@@ -378,8 +378,8 @@ int mom_mx_tree_attention(const void *q, int64_t q_stride, const int32_t *q_star
  *   out_tokens   [T] out: the tokens taken, and behind them the next token
  *   counts       [B] out: rows that stay, at least 1, and so many tokens; 0 for a sequence without rows.  What is left of rows and out_tokens is -1
  * A row whose token is none of the vocabulary, or that has no parent, is not tried.  Of equal largest logits the lowest counts.  A NaN counts as -infinity, +infinity as the largest number; where
- * all logits are -infinity nothing is taken and the next token is -1.  Where refusals leave nothing (numbers of 1 or more) it is drawn from p.
- * Everything is in 64 bits from the logits on.  T rows, B and V under 2^29, 2^29 and 2^30, and what a launch holds.  Workspace 16-byte aligned.
+ * all logits are -infinity nothing is taken and the next token is -1.  Where refusals leave nothing (a child that both models rule out, numbers of 1 or more), r is p again.
+ * Everything is in 64 bits from the logits on: r is what p and q leave of one another, right to some 2^-45 of p, and under 2^-42 of p it counts as nothing.  T rows, B and V under 2^29, 2^29 and 2^30, and what a launch holds.  Workspace 16-byte aligned.
  */
 size_t mom_verify_drafts_workspace_bytes(int64_t T, int64_t B, int64_t V);
 int mom_verify_drafts(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride, int logits_bf16, int64_t V,

@@ -143,15 +143,19 @@ MOM_MX_FN size_t tree_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, in
 
 // ---- verification ---------------------------------------------------------------------------------------------------------
 
-// 2^t in 64 bits for t <= 0: t = n + f with |f| <= 1/2, Taylor's sum of 2^f = e^(f ln 2) to f^10 (the next term is under 2.2e-13 of it), and n as the exponent.  Whatever is under
-// 2^-1074 is 0, minus infinity among it.
+// 2^t in 64 bits for t <= 0: t = n + f with |f| <= 1/2, Taylor's sum of 2^f = e^(f ln 2) to f^13 (the next term is under 5e-18), and n as the exponent: off by the
+// roundings, under 4e-16.  Whatever is under 2^-1074 is 0, minus infinity among it.
 MOM_MX_FN double power_of_two(double t) {
     t = t > -1100.0 ? t : -1100.0;                      // (NaN too)
     const double n = rint(t), f = t - n;
     constexpr double kLn2 = 0.69314718055994530942;
     constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4, c5 = c4 * kLn2 / 5, c6 = c5 * kLn2 / 6, c7 = c6 * kLn2 / 7, c8 = c7 * kLn2 / 8,
                      c9 = c8 * kLn2 / 9, c10 = c9 * kLn2 / 10;
-    double y = fma(c10, f, c9);
+    constexpr double c11 = c10 * kLn2 / 11, c12 = c11 * kLn2 / 12, c13 = c12 * kLn2 / 13;
+    double y = fma(c13, f, c12);
+    y = fma(y, f, c11);
+    y = fma(y, f, c10);
+    y = fma(y, f, c9);
     y = fma(y, f, c8);
     y = fma(y, f, c7);
     y = fma(y, f, c6);
@@ -164,20 +168,93 @@ MOM_MX_FN double power_of_two(double t) {
     return ldexp(y, (int)n);
 }
 
+// 2^t for many t of either sign, t * 1024 given as d k (at most 2^31 in size): t = n + j / 1024 + f, |f| <= 1/2048: 2^(j / 1024) from a table times Taylor's sum to f^3 (the next term is under
+// 5.5e-16), n added to the exponent: right between 2^-1022 and 2^1023.  d k is never rounded, f alone is, so distances make nothing less exact.  As two factors, so that a sum takes them in one step:
+// 7 instructions in 64 bits, 3 others and a read, where power_of_two has 23 and more.  (480 rows of 128256 logits and 208 of 152064 in bf16: 43.3 and 27.2 us; 45.0 and 28.0 with 128 powers and a
+// sum to f^4, off by 1.3e-15.)
+constexpr int kPowers = 1024, kPowerBits = 10;
+struct Powers {
+    unsigned long long of[kPowers];     // the numbers' bits, less j at the place where 1024 n + j is added: that leaves n at the exponent's
+    constexpr Powers() : of() {
+        // e^(j ln 2 / 1024), Taylor's sum from its end; ln 2 as the part whose products with j are exact, and the rest
+        constexpr double kHigh = 0x1.62e42fefap-1, kLow = 0x1.cf79abc9e3b3ap-40;
+        for (int j = 0; j < kPowers; ++j) {
+            const double x = j * kHigh / kPowers;
+            double sum = 1.0;
+            for (int n = 24; n >= 2; --n) sum = 1.0 + x / n * sum;
+            sum = 1.0 + x * sum + j * kLow / kPowers * (1.0 + x * sum);
+            of[j] = __builtin_bit_cast(unsigned long long, sum) - ((unsigned long long)j << (52 - kPowerBits));
+        }
+    }
+};
+struct Power { double two, rest; };
+struct Split { uint32_t whole; double rest; };          // 1024 t to the nearest, and the power of what that leaves
+MOM_MX_FN Split split_power(double d, double k) {
+    constexpr double kStep = 0.69314718055994530942 / kPowers, kMagic = 6755399441055744.0;       // 1.5 * 2^52: added, the sum's low word is the nearest whole number
+    const double moved = fma(d, k, kMagic), f = fma(d, k, kMagic - moved);
+    double y = fma(f, kStep * kStep * kStep / 6, kStep * kStep / 2);
+    y = fma(y, f, kStep);
+    return {(uint32_t)__builtin_bit_cast(uint64_t, moved), fma(y, f, 1.0)};
+}
+MOM_MX_FN Power power(const double* table, double d, double k) {
+    const Split s = split_power(d, k);
+    const uint64_t two = __builtin_bit_cast(uint64_t, table[s.whole & (kPowers - 1)]);
+    return {__builtin_bit_cast(double, (uint64_t)((uint32_t)(two >> 32) + (s.whole << (20 - kPowerBits))) << 32 | (uint32_t)two), s.rest};
+}
+// A logit's weight by its distance from what its row's weights are relative to: 2^(d k / 1024) down to the smallest number there is, 0 under it (what is masked is minus infinity).
+struct Scale { double k, limit; };
+MOM_MX_FN Scale scale_of(double log2e_by_t, double t) { return {log2e_by_t * kPowers, t * (1100.0 * 0.69314718055994530942)}; }
+MOM_MX_FN double weight(const double* table, double d, const Scale& s) {
+    const Split x = split_power(fmin(fmax(d, -s.limit), s.limit), s.k);
+    const uint32_t j = x.whole & (kPowers - 1);
+    const uint64_t two = __builtin_bit_cast(uint64_t, table[j]);
+    const double root = __builtin_bit_cast(double, (uint64_t)((uint32_t)(two >> 32) + (j << (20 - kPowerBits))) << 32 | (uint32_t)two);
+    return d > -s.limit ? ldexp(root * x.rest, (int32_t)x.whole >> kPowerBits) : 0.0;
+}
+// The same for many logits at once, down to 2^-1000: those that are nearer to what the weights of their row are relative to than [low, high] says.
+struct Near { float low, high; };
+MOM_MX_FN Near near_of(double top, const Scale& s) {
+    const double low = top - s.limit * (1000.0 / 1100.0), high = top + s.limit * (1000.0 / 1100.0);
+    Near n = {low < -3.402823466e38 ? -3.402823466e38f : (float)low, high > 3.402823466e38 ? 3.402823466e38f : (float)high};
+    if (n.low < low) n.low = nextafterf(n.low, INFINITY);
+    if (n.high > high) n.high = nextafterf(n.high, -INFINITY);
+    return n;
+}
+MOM_MX_FN double near_weight(const double* table, float x, double top, const Near& n, double k) {
+    const Power y = power(table, (double)fminf(fmaxf(x, n.low), n.high) - top, k);
+    return x >= n.low ? y.two * y.rest : 0.0;           // (NaN as minus infinity)
+}
+// A rest under this part of p counts as nothing.  p and q are each off by 5.5e-16 by the power's sum and by the roundings of a hundred additions at most, 1.2e-14, so what both leave of one another is off by
+// 2.5e-14 of p; that would be the whole of what is drawn from where the rest is no larger.
+constexpr double kNothing = 1.0 / ((int64_t)1 << 42);
+
 constexpr int kChunk = 4096;                            // logits of a row that a workgroup sums at once
 constexpr int64_t kMostVocabulary = (int64_t)1 << 30;
 MOM_MX_FN int64_t chunks(int64_t V) { return (V + kChunk - 1) / kChunk; }
 
 // What lies in the workspace of a verification: sums of the chunks of each row of both models and of what is left there, then what is known of a row.
-struct Part { double sum; float most; int32_t place; };                 // of a chunk: its largest logit and that one's place, sum of 2^((l - most) k)
+struct Part { double sum; float most; int32_t place; };                 // of a chunk: sum of 2^((l - most) k), most being its row's first logit, or its own largest; greedy: that and its place
 struct Row {
     double target_top, target_inverse;                  // probabilities of the target here: 2^((l - top) k) inverse
     double draft_top, draft_inverse;
     double p, q;                                        // probabilities of this row's token at the row above
-    double cut, rest;                                   // what is left here is max(p - cut q, 0) / rest
+    double cut, rest;                                   // what is left here is max(p - cut q, 0) / rest; cut 0: p
     int32_t rank, verdict, place, left;                 // which child it is; kOpen ...; the target's largest logit; refused children that `cut` counts
     int32_t again, held;                                // an earlier child of the same row is the same token; where a workgroup has its chunks' rests
 };
+// What is left of a token's probability at a row, not divided by the rest.  All that has to agree takes it from here: with the same roundings on both sides equal rows leave nothing, and a chunk whose rest is
+// above 0 has a token whose is.
+struct Left {
+    Near target, drafted;
+    double target_top, target_inverse, draft_top, draft_inverse, cut, k;
+};
+MOM_MX_FN Left left_of(const Row& r, const Scale& s) {
+    return {near_of(r.target_top, s), near_of(r.draft_top, s), r.target_top, r.target_inverse, r.draft_top, r.draft_inverse, r.cut, s.k};
+}
+MOM_MX_FN double left(const double* table, const Left& l, float target, float drafted) {
+    const double p = near_weight(table, target, l.target_top, l.target, l.k) * l.target_inverse, q = near_weight(table, drafted, l.draft_top, l.drafted, l.k) * l.draft_inverse;
+    return fmax(fma(-l.cut, q, p), 0.0);
+}
 constexpr int kOpen = 0, kTaken = 1, kRefused = 2, kPassed = 3;         // kPassed: not tried
 struct Layout { size_t target, draft, rest, rows, lists, bytes; };
 MOM_MX_FN Layout layout(int64_t T, int64_t B, int64_t V) {
