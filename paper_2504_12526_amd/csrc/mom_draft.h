@@ -239,8 +239,9 @@ struct Row {
     double draft_top, draft_inverse;
     double p, q;                                        // probabilities of this row's token at the row above
     double cut, rest;                                   // what is left here is max(p - cut q, 0) / rest; cut 0: p
-    int32_t rank, verdict, place, left;                 // which child it is; kOpen ...; the target's largest logit; refused children that `cut` counts
-    int32_t again, held;                                // an earlier child of the same row is the same token; where a workgroup has its chunks' rests
+    int32_t rank, verdict, place, left;                 // which child it is; kOpen ...; the target's largest logit; refused children that `cut` counts, without a drafting model the row from which on they
+                                                        // are taken off
+    int32_t again, held;                                // the last child of the same row before it that is the same token, 0: none; where a workgroup has its chunks' rests
 };
 // What is left of a token's probability at a row, not divided by the rest.  All that has to agree takes it from here: with the same roundings on both sides equal rows leave nothing, and a chunk whose rest is
 // above 0 has a token whose is.

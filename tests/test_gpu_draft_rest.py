@@ -98,7 +98,7 @@ def test_a_draft_that_agrees_with_the_target(V, bf16, t):
 
 
 @pytest.mark.parametrize("V", [9, 9001])
-@pytest.mark.parametrize("drafted", [True])
+@pytest.mark.parametrize("drafted", [True, False])
 def test_rows_of_one_token(V, drafted):
     """A probability of 1 and numbers of 1 and more: refused, nothing is left, and it is drawn from p."""
     B, hot = 6, [3, V - 1, 0, V // 2, 5, 1]
@@ -179,3 +179,31 @@ def test_a_child_after_refusals_that_leave_next_to_nothing():
     for b in range(B):
         assert counts[b] == (2 if b % 2 else 1) and out[3 * b] == int(peaks[b])
         assert rows[3 * b:3 * b + 3] == ([0, 2, -1] if b % 2 else [0, -1, -1])
+
+
+@pytest.mark.parametrize("chunked", [False, True])
+def test_tokens_taken_off_without_a_drafting_model(chunked):
+    """What the refused tokens leave is summed without them where little is left: few tokens among many that are masked, and tokens far below the refused one."""
+    gen, B = _gen(32), 40
+    V = 20000 if chunked else 600
+    target = torch.full((4 * B, V), -math.inf)
+    tokens, uniforms = torch.zeros(4 * B, dtype=torch.int32), torch.rand(4 * B, generator=gen)
+    for b in range(B):
+        r, places = 4 * b, torch.randperm(V, generator=gen)[:5].sort()[0]
+        if chunked:
+            places = 4096 * torch.arange(5) + torch.randint(0, 3600, (5,), generator=gen)        # a chunk each
+        if b % 2:
+            target[r, places] = torch.tensor([0.1, 1.7, 0.9, 1.3, -0.4])
+            tokens[r + 1:r + 4] = places[:3] if b % 4 == 1 else places[[2, 2, 4]]
+            uniforms[r + 1:r + 4] = 0.995
+        else:
+            target[r] = torch.randn(V, generator=gen)
+            target[r, places[0]] = 3.0 + 0.5 * b                          # all but 1e-9 of it at the most
+            tokens[r + 1:r + 4] = int(places[0])
+            uniforms[r + 1:r + 4] = 1.0
+        if b % 8 > 4:
+            uniforms[r] = 0.0
+    parents, starts = _ints([-1, 0, 0, 0] * B), [4 * b for b in range(B + 1)]
+    for children in (1, 2, 3):
+        want = dref.verify(target, None, tokens, parents, children, starts, None, uniforms)
+        _same(_verify(target, tokens, uniforms, B, None, parents, children), want)
