@@ -104,7 +104,7 @@ MOM_MX_FN AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, 
     p.whole = reach <= (p.tiles >= kManyTiles ? kManyWholeTokens : kWholeTokens) || p.tiles >= p.workgroups * Hkv || p.numbers >= 2 * p.workgroups;
     return p;
 }
-// Shares of a tile of `steps` (at least 1, under 2^24) that are no longer than `share`.
+// Shares of a tile of `steps` (at least 1, at most 2^24 + 1) that are no longer than `share`.
 MOM_MX_FN uint32_t shares_of(uint32_t steps, uint32_t share) {
     uint32_t q = (uint32_t)((float)steps * (1.0f / (float)share));       // two roundings: the quotient cut off, or one less
     q += q * share < steps;
@@ -117,14 +117,17 @@ struct ShareCount {
     uint32_t share;
     template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles * shares_of(x.steps, share); }
 };
-struct StepCount { template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles * x.steps; } };
+struct RoundCount {                                     // (in `wk` steps, which 32 bits hold for 2047 tiles of 2^29 tokens)
+    uint32_t wk;
+    template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles * ((x.steps + wk - 1) / wk); }
+};
 struct TileCount { template <typename X> MOM_MX_FN uint32_t operator()(const X& x) const { return x.tiles; } };
 template <typename Sum>
 MOM_MX_FN uint32_t shortest_share(uint32_t workgroups, uint32_t most, uint32_t wk, const Sum& sum) {
-    const uint32_t steps = sum(StepCount()), tiles = sum(TileCount());
-    uint32_t lo = (steps / workgroups + wk - 1) / wk, hi = (most + wk) / wk;
+    const uint32_t rounds = sum(RoundCount{wk}), tiles = sum(TileCount());
+    uint32_t lo = rounds / workgroups, hi = (most + wk) / wk;
     // a tile makes a share of its own and one for every whole share in it at most: so many steps are enough
-    if (tiles < workgroups && steps / (workgroups - tiles) / wk + 1 < hi) hi = steps / (workgroups - tiles) / wk + 1;
+    if (tiles < workgroups && rounds / (workgroups - tiles) + 1 < hi) hi = rounds / (workgroups - tiles) + 1;
     if (lo < 1) lo = 1;
     while (lo < hi) {
         const uint32_t mid = (lo + hi) / 2;
