@@ -50,3 +50,59 @@ def test_starts_that_do_not_ascend_reach_nothing_out_of_range(starts):
     small, other = target[:40, :3000].cpu(), draft[:40, :3000].cpu()
     t, p, u = (tokens[:40] % 3000).cpu(), _ints(_tree(rng, 40, 5)), uniforms[:40].cpu()
     _same(_verify(small.contiguous(), t, u, 1, other.contiguous(), p, 3), dref.verify(small, other, t, p, 3, [0, 40], None, u))
+
+
+def _deep(rng, m, kind):
+    if kind == "chain":
+        return list(range(-1, m - 1))
+    if kind == "star":
+        return [-1] + [rng.randrange(0, 3) for _ in range(m - 1)]
+    if kind == "far":                                                     # ways up that skip whole blocks of rows, several roots, parents that are none
+        return [rng.choice([-1, i - 1, i // 2, max(0, i - 300), i, 7]) if i % 97 else i + 5 for i in range(m)]
+    return [-1 if i == 0 else rng.randrange(max(0, i - 3), i) for i in range(m)]
+
+
+@pytest.mark.parametrize("counts,kind,words", [
+    ([513], "chain", 16), ([3000, 2, 700], "deep", 16), ([2100, 512, 511], "far", 16), ([5000], "star", 3), ([1024, 768], "far", 1), ([4001], "chain", 2),
+])
+def test_trees_of_more_rows_than_masks_know(counts, kind, words):
+    """What lies behind is climbed in steps that do not grow with the depth: masks and positions together, and each alone."""
+    rng, T = random.Random(3), sum(counts) + 2
+    parents = _ints([9] + [p for m in counts for p in _deep(rng, m, kind)] + [9])
+    starts = [1]
+    for m in counts:
+        starts.append(starts[-1] + m)
+    lens = _ints([m + 11 for m in counts])
+    # what lies above: rows before this one, so their answers are there
+    want_masks, want_positions = [[77] * words for _ in range(T)], [77] * T
+    for b, (lo, hi) in enumerate(dref.spans(starts, T)):
+        seen, depth = {}, {}
+        for i in range(hi - lo):
+            up = dref.above(parents, lo, i)
+            seen[i] = seen.get(up, 0) | (1 << i if i < 32 * words else 0)
+            depth[i] = depth.get(up, -1) + 1
+            want_masks[lo + i], want_positions[lo + i] = [seen[i] >> 32 * w & 0xffffffff for w in range(words)], int(lens[b]) - (hi - lo) + depth[i]
+    args = dict(parents=parents.to(DEV), q_starts=_ints(starts).to(DEV))
+    fresh = lambda *s: torch.full(s, 77, dtype=torch.int32, device=DEV)
+    masks, positions, alone, by_itself = fresh(T, words), fresh(T), fresh(T, words), fresh(T)
+    binding.mom_mx_tree(lens.to(DEV), masks=masks, positions=positions, **args)
+    binding.mom_mx_tree(lens.to(DEV), masks=alone, **args)
+    binding.mom_mx_tree(lens.to(DEV), positions=by_itself, **args)
+    assert [[w & 0xffffffff for w in r] for r in masks.tolist()] == want_masks and positions.tolist() == want_positions
+    assert torch.equal(alone, masks) and torch.equal(by_itself, positions)
+
+
+@pytest.mark.parametrize("listed", [True, False])
+def test_a_chain_of_a_whole_prompt_and_a_tree_as_long(listed):
+    m = 1 << 20
+    lens = _ints([m + 5]).to(DEV)
+    masks, positions = torch.full((m, 16), 77, dtype=torch.int32, device=DEV), torch.full((m,), 77, dtype=torch.int32, device=DEV)
+    for parents in (None, torch.arange(-1, m - 1, dtype=torch.int32, device=DEV)):
+        masks.fill_(77)
+        positions.fill_(77)
+        binding.mom_mx_tree(lens, parents=parents, q_starts=_ints([0, m]).to(DEV) if listed else None, masks=masks, positions=positions)
+        assert torch.equal(positions, torch.arange(5, m + 5, dtype=torch.int32, device=DEV))
+        i, j = torch.arange(m, device=DEV)[:, None], torch.arange(16, device=DEV) * 32
+        bits = (i + 1 - j).clamp(0, 32)
+        want = torch.where(bits == 32, -1, (1 << bits.clamp(max=31)) - 1).to(torch.int32)
+        assert torch.equal(masks, torch.where(bits == 32, torch.full_like(want, -1), want))
