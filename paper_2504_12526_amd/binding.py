@@ -545,10 +545,10 @@ def mom_verify_drafts_workspace_bytes(T, B, V):
     return int(lib().mom_verify_drafts_workspace_bytes(int(T), int(B), int(V)))
 
 
-def mom_verify_drafts(target, tokens, uniforms, rows, out_tokens, counts, workspace, draft=None, parents=None, max_children=1, q_starts=None, temperatures=None,
+def mom_verify_drafts(target, tokens, uniforms, rows, out_tokens, counts, workspace, draft=None, parents=None, max_children=None, q_starts=None, temperatures=None,
                       stream=None, check=True):
-    """Which of the drafted tokens [T] int32 stay: target and draft [T, V] logits (rows may lie apart), uniforms [T] fp32, parents [T] int32 (None: chains), temperatures [B] fp32
-    (None: 1).  rows, out_tokens [T] and counts [B] int32 out; workspace any device tensor of at least mom_verify_drafts_workspace_bytes bytes."""
+    """Which of the drafted tokens [T] int32 stay: target and draft [T, V] logits (rows may lie apart), uniforms [T] fp32, parents [T] int32 (None: chains), max_children how
+    many children of a row are tried (to be given with parents; a chain has one), temperatures [B] fp32 (None: 1).  rows, out_tokens [T] and counts [B] int32 out; workspace any device tensor of at least mom_verify_drafts_workspace_bytes bytes."""
     T, V = target.shape
     B = counts.shape[0]
     target_stride = _logits("target", target)
@@ -559,6 +559,10 @@ def mom_verify_drafts(target, tokens, uniforms, rows, out_tokens, counts, worksp
     _starts(q_starts, T, B)
     if temperatures is not None:
         _dense("temperatures", temperatures, torch.float32, (B,))
+    if max_children is None:
+        if parents is not None:
+            raise ValueError("max_children must say how many children of a row are tried")
+        max_children = 1
     rc = lib().mom_verify_drafts(_ptr(target), target_stride, _ptr(draft), draft_stride, int(target.dtype == torch.bfloat16), V, _ptr(tokens), _ptr(parents), int(max_children),
                                  _ptr(q_starts), T, B, _ptr(temperatures), _ptr(uniforms), _ptr(rows), _ptr(out_tokens), _ptr(counts), _ptr(workspace), _nbytes(workspace),
                                  _stream(stream))
