@@ -351,7 +351,8 @@ int mom_mx_tree(const int32_t *parents, const int32_t *q_starts, int64_t T, int6
  * trees'; a row whose mask is empty sees what is in front, and is 0 with lse -infinity where that is nothing).
  *   masks, mask_words   as mom_mx_tree writes them; rows past the last word are not seen
  *   window       0, or how many tokens a row sees at most: the last ones, in the order of the cache, of those that it would see
- * Everything else as in mom_mx_attention, the workspace by this call's own query.  What the weights lose by their rounding is multiplied too where tiles have 16 rows (few rows, or little to do)
+ * Everything else as in mom_mx_attention, the workspace by this call's own query: what is asked for one call is enough for all of no more rows, sequences and tokens, and at most
+ * 4 (head_dim + 2) (8192 + 32 kv_heads) bytes.  What the weights lose by their rounding is multiplied too where tiles have 16 rows (few rows, or little to do)
  * and are fewer than 64; the device cuts tokens into shares by the lengths that it finds, so the bits of a sequence depend on the call that it is in.
  */
 size_t mom_mx_tree_attention_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_kv);

@@ -86,6 +86,8 @@ constexpr int64_t kLittle = 65536;                      // tokens, of all tiles 
 // Whole tiles: a second launch joins shares, 5 us.  8 tiles of 32 rows and 1024 tokens take 12.7 us whole and 13.5 in shares, 1536 tokens 15.5 and 13.8; 64 tiles of 1024 12.9 and 16.9; as many tiles
 // as workgroups at once, of lengths up to 8192, 50.6 and 57.7.
 constexpr int kWholeTokens = 1024, kManyWholeTokens = 1536, kManyTiles = 64, kAtOnce = 256;
+// Workgroups of a key head, so that there are as many of all heads as the compute units hold at once.
+MOM_MX_FN int64_t workgroups_at_once(int qb, int Hkv, int D) { return (kAtOnce * (qb == 1 && D <= 128 ? 2 : 1) + Hkv - 1) / Hkv; }
 MOM_MX_FN AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv, int64_t window, bool listed) {
     const int group = Hq / Hkv;
     const int64_t average = (T * group + B - 1) / B, rows = listed ? T : T / B;
@@ -98,9 +100,7 @@ MOM_MX_FN AttentionPlan tree_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, 
     const int64_t even = B * ((average + p.rows - 1) / p.rows), uneven = (2 * T * group + (B + 1) * p.rows - 1) / (2 * p.rows);
     p.tiles = (!listed ? even : uneven < B ? B : uneven) * Hkv;
     p.numbers = listed ? mx::tile_numbers(T, B, group, p.rows) : even;
-    // of all heads as many as the compute units hold at once
-    const int64_t at_once = kAtOnce * (p.qb == 1 && D <= 128 ? 2 : 1);
-    p.workgroups = (at_once + Hkv - 1) / Hkv;
+    p.workgroups = workgroups_at_once(p.qb, Hkv, D);
     p.whole = reach <= (p.tiles >= kManyTiles ? kManyWholeTokens : kWholeTokens) || p.tiles >= p.workgroups * Hkv || p.numbers >= 2 * p.workgroups;
     return p;
 }
@@ -138,10 +138,17 @@ MOM_MX_FN uint32_t shortest_share(uint32_t workgroups, uint32_t most, uint32_t w
 }
 MOM_MX_FN int64_t plan_workgroups(const AttentionPlan& p) { return p.whole || p.numbers > p.workgroups ? p.numbers : p.workgroups; }
 MOM_MX_FN size_t plan_workspace(const AttentionPlan& p, int Hkv, int D) { return p.whole ? 0 : (size_t)p.workgroups * Hkv * p.rows * (D + 2) * 4; }
-// (Fewer tokens or a window may have tiles of 16 rows where more have 32: twice the workgroups, half the rows, and the same bytes.)
-MOM_MX_FN size_t tree_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D, int64_t max_kv) {
-    const size_t even = plan_workspace(tree_plan(T, B, Hq, Hkv, D, max_kv, 0, false), Hkv, D), uneven = plan_workspace(tree_plan(T, B, Hq, Hkv, D, max_kv, 0, true), Hkv, D);
-    return even > uneven ? even : uneven;
+// That of all calls of no more rows, sequences and tokens (fewer tiles are cut where more are whole), with any window: of either height of tiles.
+MOM_MX_FN size_t tree_workspace(int64_t, int64_t, int, int Hkv, int D, int64_t max_kv) {
+    if (max_kv <= kWholeTokens) return 0;
+    size_t most = 0;
+    for (int qb = 1; qb <= 2; ++qb) {
+        AttentionPlan p = {};
+        p.rows = 16 * qb, p.workgroups = workgroups_at_once(qb, Hkv, D);
+        const size_t bytes = qb == 2 && D == 256 ? 0 : plan_workspace(p, Hkv, D);
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 // ---- verification ---------------------------------------------------------------------------------------------------------

@@ -1,4 +1,4 @@
-// Walks on the CPU what mom_draft.h says at the largest extents that the calls take: shares of sequences of up to 2^29 tokens.
+// Walks on the CPU what mom_draft.h says at the largest extents that the calls take: shares of sequences of up to 2^29 tokens, and the workspace of all calls that are no larger than one.
 #include "mom_draft.h"
 
 #include <stdio.h>
@@ -64,7 +64,27 @@ static void check_shares() {
     CHECK(cuts > 3000, "cuts %d", cuts);
 }
 
+// One buffer for a server's calls: what the largest has asked for is enough where sequences end, rows are fewer, or the window or the cache is shorter.
+static void check_workspace() {
+    int some = 0;
+    for (int k = 0; k < 40000; ++k) {
+        const int heads[][2] = {{32, 8}, {28, 4}, {16, 1}, {1, 1}, {8, 8}, {64, 64}};
+        const int* h = heads[upto(5)];
+        const int D = 64 << upto(2);
+        const int64_t B = 1 + upto(upto(1) ? 300 : 20), T = B * (1 + upto(upto(1) ? 8 : 200)), max_kv = upto(upto(1) ? 9000 : 200000);
+        const int64_t b = 1 + upto(B - 1), most = 1 + upto(T - 1), t = upto(1) ? most : most < b ? b : most / b * b, kv = upto(1) ? max_kv : upto(max_kv), window = upto(2) ? 0 : 1 + upto(5000);
+        const bool listed = t % b ? true : upto(1);
+        if (t > T) continue;
+        const size_t need = draft::plan_workspace(draft::tree_plan(t, b, h[0], h[1], D, kv, window, listed), h[1], D), has = draft::tree_workspace(T, B, h[0], h[1], D, max_kv);
+        CHECK(need <= has, "workspace of T %d B %d kv %d in that of T %d B %d kv %d: heads %d %d, D %d, window %d", (int)t, (int)b, (int)kv, (int)T, (int)B, (int)max_kv, h[0], h[1], D, (int)window);
+        CHECK(has <= (size_t)4 * (D + 2) * (8192 + 32 * h[1]), "workspace");
+        some += need > 0;
+    }
+    CHECK(some > 10000, "workspaces %d", some);
+}
+
 int main() {
+    check_workspace();
     check_shares();
     printf("draft_limits_check: ok\n");
     return 0;

@@ -15,12 +15,14 @@ def _check(tmp_path, include):
     return subprocess.run([exe], capture_output=True, text=True, timeout=60)
 
 
-def test_shares_of_the_longest_sequences(tmp_path):
+def test_shares_of_the_longest_sequences_and_one_workspace_for_smaller_calls(tmp_path):
     r = _check(tmp_path, CSRC)
     assert r.returncode == 0 and ": ok" in r.stdout, r.stdout
 
 
 @pytest.mark.parametrize("old,new,says", [
+    ("for (int qb = 1; qb <= 2; ++qb) {", "for (int qb = 2; qb <= 2; ++qb) {", "workspace"),
+    ("if (max_kv <= kWholeTokens) return 0;", "if (max_kv <= kManyWholeTokens) return 0;", "workspace"),
     ("return x.tiles * ((x.steps + wk - 1) / wk); }", "return x.tiles * x.steps; }", "shortest"),
     ("hi = rounds / (workgroups - tiles) + 1;", "hi = rounds / workgroups + 1;", "room"),
     ("uint32_t lo = rounds / workgroups,", "uint32_t lo = rounds / workgroups + 3,", "shortest"),
