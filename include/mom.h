@@ -390,7 +390,7 @@ int mom_verify_drafts(const void *target, int64_t target_stride, const void *dra
 
 /*
  * The rows that stay moved together in a layer's cache: token n - m + rows[i] of sequence b goes to the place n - m + i, for i under counts[b] (at most m).
- * rows and counts as mom_verify_drafts writes them: rising, and no row lower than its place (a row that is neither, or none of the sequence's, is not moved; nothing out of range is
+ * rows and counts as mom_verify_drafts writes them: rising, so that no row is lower than its place (one that is, or is none of the sequence's, is not moved; nothing out of range is
  * touched).  Tokens whose place or page is none of the cache's stay, too.
  *   page_table, table_stride, page_tokens, max_kv, kv_lens   as before the call: the rows among the tokens
  *   new_lens     [B] out: n - m + counts[b], what the cache holds of the sequence now; another buffer than kv_lens, which the other layers' calls still need

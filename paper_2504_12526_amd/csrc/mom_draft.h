@@ -1,5 +1,5 @@
 // Drafted tokens in a tree: what a row sees, how the logits are cut into chunks and where their sums lie, and the power of two in 64 bits, as kernels
-// (mom_draft.hip.inc, mom_mx_attention.hip.inc), entry points and a host program (tests/draft_check.cpp) ask.  Plain C++17, no HIP types.
+// (mom_draft.hip.inc, mom_draft_attention.hip.inc), entry points and host programs (tests/draft_*check.cpp) ask.  Plain C++17, no HIP types.
 //
 // The rows of a sequence are its m new tokens: row i is token n - m + i of the n in the cache.  Bit j of a row's mask says that it sees row j.
 #ifndef MOM_DRAFT_H
